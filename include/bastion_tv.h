@@ -11,7 +11,7 @@
  *     call of another kind would write over that or take its own data for it.  The kinds:
  *       tree build in all its forms | attention in all its forms and the ancestor mask |
  *       greedy acceptance of one request | stochastic acceptance | acceptance from hidden states |
- *       greedy acceptance of a batch | KV commit
+ *       greedy acceptance of a batch | KV commit | paged_extend and rope_append
  *     Every call leaves its workspace ready for the next one of its kind, of any size that the
  *     workspace holds (the data flag aside, see btv_workspace_status).  To give a workspace to
  *     another kind, zero-fill it again.  A workspace serves one call at a time.
@@ -396,6 +396,100 @@ int btv_kv_commit_paged(void *Kpool, void *Vpool, int layers, long long layer_st
                         const int32_t *block_table, int max_blocks, const int32_t *prefix_len,
                         const int32_t *path, const int32_t *q_offset, int total_M, const int32_t *n_acc,
                         int batch, int M_max, int row_bytes, int32_t *new_len, void *ws, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Rows that a paged cache takes in: their pages and slots, their rotation and the append, and the
+ * attention of a prompt's rows.  One step of a batch is paged_extend -> (per layer: the caller's
+ * projections, rope_append, attention); tree_verify_attn_paged takes the same tables for the draft
+ * trees.  Pages hold BTV_PAGE rows; row j of request r lies in slot
+ *   block_table[r][j / BTV_PAGE] * BTV_PAGE + j % BTV_PAGE  of the pools.
+ *
+ * paged_extend -- request r has prefix_len[r] = L_r rows in its first ceil(L_r / BTV_PAGE) pages,
+ * holds n_pages[r] = P_r >= that many, and gets n_new[r] = M_r >= 0 rows more.  It takes
+ *   t_r = max(0, ceil((L_r + M_r) / BTV_PAGE) - P_r)  pages off the free list, in the order of the
+ * requests: take number k of the batch is free_pages[*n_free - 1 - k].  A request whose last take
+ * lies past the end of the list gets none of them (nor does a later one that needs any).
+ *   depth        [>= total] optional: as written by tree_build(_batch); 1-based depths of the new rows
+ *   free_pages   [num_blocks] page ids, the first *n_free of them valid;  n_free [1]
+ *   block_table  [batch, max_blocks], in place: entries P_r .. P_r + t_r - 1 of row r
+ *   q_offset     [batch + 1]: sums of M_r (2^31 - 1 at most), the array that the batch calls take
+ *   slot, position  [total_max]: of new row q_offset[r] + i.  position = L_r + i, or with depth
+ *                L_r + depth - 1.  slot -1 and position 0: the request did not get its pages, or the row
+ *                is past the last request's; rope_append passes such rows over.
+ *   n_pages_out  [batch] = P_r + t_r, n_free_out [1]; neither may be its input.
+ * Pages stay with a request until the caller puts them back: behind the free list's last valid
+ * entry, *n_free raised.  ws (optional, BTV_WS_HEADER's 256 bytes) receives the data flag: a request
+ * without its pages or with lengths out of range (counted as M_r rows, or 0 if that is negative),
+ * more than total_max rows (the surplus has no entry), page ids outside [0, num_blocks) (slot -1).
+ * 1 <= batch <= 4096.
+ * ------------------------------------------------------------------------------------------- */
+int btv_paged_extend(const int32_t *prefix_len, const int32_t *n_new, const int32_t *depth, int batch,
+                     int total_max, const int32_t *n_pages, const int32_t *free_pages,
+                     const int32_t *n_free, int num_blocks, int32_t *block_table, int max_blocks,
+                     int32_t *q_offset, int32_t *slot, int32_t *position, int32_t *n_pages_out,
+                     int32_t *n_free_out, void *ws, void *stream);
+
+/* rope_append -- rotary positions of the rows' queries and keys, and the append of keys and values to
+ * the cache, in one pass.  The first R channels of a head form R/2 pairs: (i, i + R/2), or with
+ * interleaved = 1 (2i, 2i + 1).  Pair i of a row at position n turns by t = n * inv_freq[i]:
+ *   a' = factor * (a cos t - b sin t),  b' = factor * (a sin t + b cos t);
+ * channels from R on stay as they are.  t is formed and reduced in fp64, the rotation is in fp32.
+ *   Q, K, V      rows of [Hq, D], [Hkv, D], [Hkv, D] of `dtype`, q_stride, k_stride, v_stride ELEMENTS
+ *                apart (a projection's packed output is read where it lies); 16-byte aligned rows
+ *   position, slot  [total], as paged_extend writes them.  Rows of a slot < 0 are not stored in the
+ *                cache (their queries are rotated all the same).  No two rows may have one slot: it
+ *                would hold either row, or parts of both.
+ *   inv_freq     [R/2] fp64 DEVICE, radians per position;  R a multiple of 16, 0 <= R <= D
+ *   Qout         [total, Hq, D] of `dtype`; may be Q where q_stride = Hq * D
+ *   Kcache, Vcache  [num_slots, Hkv, D] of `dtype`: the pools of a paged cache (num_slots = num_blocks *
+ *                BTV_PAGE), or a contiguous one (slot = row).  They may not overlap Q, K or V.
+ * fp8kv: dtype bf16, caches of E4M3 codes: x / scale, limited to +-448, to nearest even (NaN stays NaN).
+ * ws (optional) receives the data flag for a slot >= num_slots; that row is passed over.
+ *
+ * rope_frequencies -- HOST function: inv_freq [R/2] HOST and the factor.  w_i = theta^(-2i/R) is
+ *   PLAIN   taken as it is             LINEAR  divided by stretch (>= 1)
+ *   NTK     of theta * stretch^(R/(R-2))
+ *   PARTS   kept where a context of `original` positions has `high` turns or more, divided by stretch
+ *           where it has `low` or fewer, and weighted linearly in the turns between
+ *   YARN    as PARTS, with factor = 0.1 ln(stretch) + 1 (1 in the other forms)
+ * Arguments that a form does not use are not looked at. */
+enum { BTV_ROPE_PLAIN = 0, BTV_ROPE_LINEAR = 1, BTV_ROPE_NTK = 2, BTV_ROPE_PARTS = 3, BTV_ROPE_YARN = 4 };
+int btv_rope_append(const void *Q, long long q_stride, const void *K, long long k_stride, const void *V,
+                    long long v_stride, int dtype, int total, int Hq, int Hkv, int D,
+                    const int32_t *position, const int32_t *slot, const double *inv_freq, int R,
+                    int interleaved, float factor, void *Qout, void *Kcache, void *Vcache,
+                    long long num_slots, void *ws, void *stream);
+int btv_rope_append_fp8kv(const void *Q, long long q_stride, const void *K, long long k_stride,
+                          const void *V, long long v_stride, int total, int Hq, int Hkv, int D,
+                          const int32_t *position, const int32_t *slot, const double *inv_freq, int R,
+                          int interleaved, float factor, void *Qout, void *K8cache, void *V8cache,
+                          float k_scale, float v_scale, long long num_slots, void *ws, void *stream);
+int btv_rope_frequencies(int R, double theta, int scaling, double stretch, double original, double low,
+                         double high, double *inv_freq, double *factor);
+
+/* chunk_attn_paged -- causal attention of the requests' new rows over their pages: prompts, chunks of
+ * them, single tokens, in one ragged batch.  Row i of request r sees the keys of its positions
+ * 0 .. prefix_len[r] + i (itself included; its K/V rows lie in the pages already).
+ *   Q, O [total_M, Hq, D] bf16; request r owns rows q_offset[r] .. q_offset[r+1]-1, any number of them,
+ *        0 included; rows of O that no request owns are left as they are.  Q may have more rows than
+ *        the requests own (a padded batch); with none at all the call does nothing
+ *   Kpool, Vpool, num_blocks, block_table, max_blocks, q_offset, prefix_len, Hq, Hkv, D, scale: as for
+ *        btv_tree_verify_attn_paged; 1 <= batch <= 4096
+ *   M_max, L_max  HOST upper bounds of a request's new rows (1 <= M_max <= 2^20) and of its prefix; a
+ *        request that exceeds them, or max_blocks * BTV_PAGE, is passed over and flagged
+ * The workspace is of the attention kind; the query answers what every call with no larger batch,
+ * M_max and L_max needs.  fp8kv: as there, D = 128. */
+size_t btv_chunk_attn_paged_workspace(int batch, int M_max, int L_max, int Hq, int Hkv, int D);
+int btv_chunk_attn_paged(const void *Q, const void *Kpool, const void *Vpool, int num_blocks,
+                         const int32_t *block_table, int max_blocks, const int32_t *q_offset,
+                         const int32_t *prefix_len, int batch, int total_M, int M_max, int L_max, int Hq,
+                         int Hkv, int D, float scale, void *O, void *ws, size_t ws_bytes, void *stream);
+size_t btv_chunk_attn_paged_fp8kv_workspace(int batch, int M_max, int L_max, int Hq, int Hkv, int D);
+int btv_chunk_attn_paged_fp8kv(const void *Q, const void *K8pool, const void *V8pool, float k_scale,
+                               float v_scale, int num_blocks, const int32_t *block_table, int max_blocks,
+                               const int32_t *q_offset, const int32_t *prefix_len, int batch, int total_M,
+                               int M_max, int L_max, int Hq, int Hkv, int D, float scale, void *O, void *ws,
+                               size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Tuning and test form of btv_tree_verify_attn / btv_tree_verify_attn_fp8kv (App. C; bf16 Q and O):

@@ -332,3 +332,53 @@ def kv_commit(cache: np.ndarray, L: int, M: int, path, block_table=None, page: i
     if rc < 0:
         raise ValueError("orc_kv_commit: bad arguments")
     return int(rc)
+
+
+# ---- rows that a paged cache takes in: straight from the definitions, in Python ----------------------------------------------
+
+def paged_extend(prefix_len, n_new, n_pages, free_pages, n_free: int, table: np.ndarray, total_max: int, depth=None, page: int = 16) -> dict:
+    """Pages, slots and positions of the requests' next rows, one request after the other.  `table` is copied."""
+    table = np.array(table, dtype=np.int32)
+    slot, position = np.full(total_max, -1, dtype=np.int32), np.zeros(total_max, dtype=np.int32)
+    num_blocks = len(free_pages)
+    bad = not 0 <= n_free <= num_blocks
+    left = n_free = 0 if bad else int(n_free)
+    offset, pages_out, wanted = [0], [], 0
+    for r, (L, M, P) in enumerate(zip(map(int, prefix_len), map(int, n_new), map(int, n_pages))):
+        ok = L >= 0 and M >= 0 and L + M <= table.shape[1] * page and -(-L // page) <= P <= table.shape[1]
+        take = max(0, -(-(L + M) // page) - P) if ok else 0
+        wanted += take
+        granted = ok and (take == 0 or wanted <= n_free)
+        bad = bad or not granted
+        if granted:
+            for k in range(take):
+                left -= 1
+                table[r, P + k] = free_pages[left]
+        for i in range(max(M, 0)):
+            row = offset[-1] + i
+            if row >= total_max:
+                bad = True
+                break
+            if granted:
+                position[row] = L + (i if depth is None else int(depth[row]) - 1)
+                p = int(table[r, (L + i) // page])
+                if 0 <= p < num_blocks:
+                    slot[row] = p * page + (L + i) % page
+                else:
+                    bad = True
+        offset.append(offset[-1] + max(M, 0))
+        pages_out.append(P + take if granted else P)
+    return {"q_offset": np.minimum(offset, 2**31 - 1).astype(np.int32), "slot": slot, "position": position, "n_pages": np.array(pages_out, dtype=np.int32),
+            "n_free": left, "table": table, "bad": bad}
+
+
+def rope(x: np.ndarray, position, inv_freq, interleaved: bool = False, factor: float = 1.0) -> np.ndarray:
+    """x [T, H, D] rotated in fp64, as complex numbers."""
+    y = np.array(x, dtype=np.float64)
+    w = np.asarray(inv_freq, dtype=np.float64)
+    n = len(w)
+    turn = factor * np.exp(1j * np.asarray(position, dtype=np.float64)[:, None] * w)[:, None, :]
+    a, b = (slice(0, 2 * n, 2), slice(1, 2 * n, 2)) if interleaved else (slice(0, n), slice(n, 2 * n))
+    z = (y[..., a] + 1j * y[..., b]) * turn
+    y[..., a], y[..., b] = z.real, z.imag
+    return y

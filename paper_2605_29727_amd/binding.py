@@ -17,6 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libbastion_tv.so")
 
 BTV_F32, BTV_BF16 = 0, 1
 BTV_MAX_NODES, BTV_MAX_DEPTH, BTV_PAGE, BTV_ANC_WORDS = 256, 16, 16, 8
+BTV_ROPE_PLAIN, BTV_ROPE_LINEAR, BTV_ROPE_NTK, BTV_ROPE_PARTS, BTV_ROPE_YARN = range(5)
 BTV_OK, BTV_EINVAL, BTV_EWORKSPACE, BTV_EHIP, BTV_EDATA = 0, -1, -2, -3, -4
 
 EXPORTS = [
@@ -32,7 +33,8 @@ EXPORTS = [
     "btv_tree_accept_greedy", "btv_tree_accept_stochastic", "btv_tree_accept_lm_head_workspace",
     "btv_tree_accept_greedy_lm_head", "btv_tree_verify_attn_tuned_workspace", "btv_tree_verify_attn_tuned",
     "btv_tree_verify_attn_noalloc", "btv_tree_verify_attn_merge_tuned", "btv_tree_build_tuned", "btv_tree_accept_greedy_tuned",
-    "btv_tree_accept_stochastic_tuned",
+    "btv_tree_accept_stochastic_tuned", "btv_paged_extend", "btv_rope_append", "btv_rope_append_fp8kv", "btv_rope_frequencies",
+    "btv_chunk_attn_paged_workspace", "btv_chunk_attn_paged", "btv_chunk_attn_paged_fp8kv_workspace", "btv_chunk_attn_paged_fp8kv",
 ]
 
 
@@ -57,7 +59,8 @@ def lib() -> C.CDLL:
                   "btv_tree_verify_attn_paged_workspace", "btv_tree_verify_attn_fp8kv_workspace",
                   "btv_tree_verify_attn_paged_fp8kv_workspace", "btv_tree_accept_workspace",
                   "btv_tree_accept_lm_head_workspace", "btv_tree_build_batch_workspace",
-                  "btv_tree_accept_batch_workspace", "btv_tree_verify_attn_tuned_workspace"):
+                  "btv_tree_accept_batch_workspace", "btv_tree_verify_attn_tuned_workspace", "btv_chunk_attn_paged_workspace",
+                  "btv_chunk_attn_paged_fp8kv_workspace"):
             getattr(L, n).restype = C.c_size_t
         for n in ("btv_version", "btv_workspace_status", "btv_tree_build", "btv_tree_build_beam", "btv_tree_ancestor_mask",
                   "btv_tree_verify_attn", "btv_tree_verify_attn_paged", "btv_tree_verify_attn_fp8kv",
@@ -113,7 +116,7 @@ def _dtype_code(t) -> int:
 def alloc_workspace(nbytes: int, device="cuda") -> torch.Tensor:
     """A zero-initialised device buffer of at least nbytes (torch allocations are 256-byte aligned).  One for each kind of
     call: tree builds, attention, greedy acceptance, stochastic acceptance, acceptance from hidden states, batch
-    acceptance (include/bastion_tv.h: what kernels keep in it from call to call does not survive a call of another kind)."""
+    acceptance, paged_extend and rope_append (include/bastion_tv.h: what kernels keep in it from call to call does not survive a call of another kind)."""
     return torch.zeros(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
 
@@ -353,3 +356,50 @@ def btv_kv_commit_paged(Kpool, Vpool, block_table, prefix_len, path, n_acc, new_
     """Kpool, Vpool [layers, num_blocks, PAGE, ...]; block_table [batch, max_blocks]; path [batch, M_max], or with
     q_offset [batch + 1] the ragged [total_M] layout of the batch acceptance (then M_max must be given)."""
     (_face or _load_face()).kv_commit_paged(Kpool, Vpool, block_table, prefix_len, path, n_acc, new_len, ws, q_offset, M_max)
+
+
+# ---------------------------------------------------------------------------------------------
+
+def btv_paged_extend(prefix_len, n_new, depth, n_pages, free_pages, n_free, block_table, q_offset, slot, position, n_pages_out, n_free_out,
+                     ws=None) -> None:
+    """Pages, slots and positions of the requests' next rows.  block_table [batch, max_blocks] is extended in place; free_pages has an entry per page of the
+    cache; slot and position may be longer than the rows are (a padded batch: slot -1 there)."""
+    (_face or _load_face()).paged_extend(prefix_len, n_new, depth, n_pages, free_pages, n_free, block_table, q_offset, slot, position, n_pages_out, n_free_out, ws)
+
+
+def btv_rope_append(Q, K, V, position, slot, inv_freq, Qout, Kcache, Vcache, interleaved: bool = False, factor: float = 1.0, ws=None) -> None:
+    """Q [total, Hq, D], K, V [total, Hkv, D]: rows may lie apart (views of a packed projection), heads and channels may not.  The caches are pools [blocks,
+    BTV_PAGE, Hkv, D] or rows [n, Hkv, D]; inv_freq [R/2] float64 on the device (btv_rope_frequencies)."""
+    (_face or _load_face()).rope_append(Q, K, V, position, slot, inv_freq, Qout, Kcache, Vcache, interleaved, factor, ws)
+
+
+def btv_rope_append_fp8kv(Q, K, V, position, slot, inv_freq, Qout, K8cache, V8cache, k_scale: float, v_scale: float, interleaved: bool = False,
+                          factor: float = 1.0, ws=None) -> None:
+    """btv_rope_append into caches of one-byte E4M3 codes."""
+    (_face or _load_face()).rope_append_fp8kv(Q, K, V, position, slot, inv_freq, Qout, K8cache, V8cache, k_scale, v_scale, interleaved, factor, ws)
+
+
+def btv_rope_frequencies(R: int, theta: float, scaling: int = BTV_ROPE_PLAIN, stretch: float = 1.0, original: float = 0.0, low: float = 1.0,
+                         high: float = 32.0) -> tuple:
+    """Host-side: (list of R/2 radians per position, factor) for btv_rope_append."""
+    out, f = (C.c_double * max(int(R) // 2, 1))(), C.c_double()
+    _check(lib().btv_rope_frequencies(int(R), C.c_double(float(theta)), int(scaling), *[C.c_double(float(x)) for x in (stretch, original, low, high)], out,
+                                      C.byref(f)))
+    return list(out), f.value
+
+
+def btv_chunk_attn_paged_workspace(batch, M_max, L_max, Hq, Hkv, D) -> int:
+    return int(lib().btv_chunk_attn_paged_workspace(batch, M_max, L_max, Hq, Hkv, D))
+
+
+def btv_chunk_attn_paged(Q, Kpool, Vpool, block_table, q_offset, prefix_len, M_max: int, L_max: int, O, ws, scale: float = 0.0) -> None:
+    (_face or _load_face()).chunk_attn_paged(Q, Kpool, Vpool, block_table, q_offset, prefix_len, M_max, L_max, O, ws, scale)
+
+
+def btv_chunk_attn_paged_fp8kv_workspace(batch, M_max, L_max, Hq, Hkv, D) -> int:
+    return int(lib().btv_chunk_attn_paged_fp8kv_workspace(batch, M_max, L_max, Hq, Hkv, D))
+
+
+def btv_chunk_attn_paged_fp8kv(Q, K8pool, V8pool, k_scale: float, v_scale: float, block_table, q_offset, prefix_len, M_max: int, L_max: int, O, ws,
+                               scale: float = 0.0) -> None:
+    (_face or _load_face()).chunk_attn_paged_fp8kv(Q, K8pool, V8pool, k_scale, v_scale, block_table, q_offset, prefix_len, M_max, L_max, O, ws, scale)

@@ -3,6 +3,7 @@
 // tensor), about what its kernels take at small sizes; here it is under one, of the 3 to 4 us that a call of one or two
 // launches takes on the host.  What is checked, and what is raised, is what binding.py does for the other calls.
 #include <torch/csrc/autograd/python_variable.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
 #include "bastion_tv.h"
@@ -403,6 +404,126 @@ FACE(kv_commit_paged)
     });
 }
 
+// What the calls below ask of their tensors: on the current device (whose current stream the call goes to), contiguous, of a type.
+template <typename T = void>
+T *typed(const at::Tensor &t, at::ScalarType type, const char *text)
+{
+    require(t.is_cuda() && t.scalar_type() == type && t.is_contiguous(), text);
+    require(t.device().index() == c10::hip::current_device(), "tensors of another device than the current one");
+    return static_cast<T *>(t.data_ptr());
+}
+int32_t *ints(const at::Tensor &t) { return typed<int32_t>(t, at::kInt, "int32 tensors must be contiguous CUDA tensors of that type"); }
+int32_t *ints(const at::Tensor &t, int64_t n)
+{
+    require(t.numel() >= n, "an int32 tensor is too short");
+    return ints(t);
+}
+void *flag_workspace(Args &a)
+{
+    const at::Tensor *t = a.tensor_or_none();
+    if (!t) return nullptr;
+    require(t->is_cuda() && t->is_contiguous() && t->device().index() == c10::hip::current_device() && t->numel() * t->element_size() >= 256,
+            "a workspace is a contiguous CUDA tensor of 256 bytes or more on the current device");
+    return t->data_ptr();
+}
+int narrow_size(int64_t v)
+{
+    if (v != (int)v) raise(PyExc_OverflowError, "a tensor's dimension is out of range");
+    return (int)v;
+}
+
+FACE(paged_extend)
+{
+    return call(args, n, [](Args &a) {
+        const at::Tensor &L = a.tensor(), &M = a.tensor();
+        const at::Tensor *d = a.tensor_or_none();
+        const at::Tensor &P = a.tensor(), &fp = a.tensor(), &nf = a.tensor(), &bt = a.tensor(), &qo = a.tensor(), &sl = a.tensor(), &po = a.tensor();
+        const at::Tensor &Po = a.tensor(), &nfo = a.tensor();
+        void *ws = flag_workspace(a);
+        dims(bt, 2);
+        const int batch = narrow_size(bt.size(0)), max_blocks = narrow_size(bt.size(1)), total_max = narrow_size(sl.numel()), num_blocks = narrow_size(fp.numel());
+        require(po.numel() == sl.numel(), "slot and position must be of one length");
+        const int32_t *prefix = ints(L, batch), *n_new = ints(M, batch), *depth = d ? ints(*d) : nullptr, *held = ints(P, batch), *pages = ints(fp), *n_free = ints(nf, 1);
+        int32_t *table = ints(bt), *q_offset = ints(qo, (int64_t)batch + 1), *slot = ints(sl), *position = ints(po), *held_out = ints(Po, batch), *n_free_out = ints(nfo, 1);
+        if (d) require(d->numel() >= total_max, "a depth for every entry of slot");
+        return [=](void *st) {
+            return btv_paged_extend(prefix, n_new, depth, batch, total_max, held, pages, n_free, num_blocks, table, max_blocks, q_offset, slot, position, held_out,
+                                    n_free_out, ws, st);
+        };
+    });
+}
+
+PyObject *append(PyObject *const *args, Py_ssize_t n, bool fp8)
+{
+    return call(args, n, [fp8](Args &a) {
+        const at::Tensor &q = a.tensor(), &k = a.tensor(), &v = a.tensor(), &po = a.tensor(), &sl = a.tensor(), &fr = a.tensor(), &qo = a.tensor();
+        const at::Tensor &kc = a.tensor(), &vc = a.tensor();
+        const float k_scale = fp8 ? (float)a.real() : 1.f, v_scale = fp8 ? (float)a.real() : 1.f;
+        const int interleaved = a.int32() != 0;
+        const float factor = (float)a.real();
+        void *ws = flag_workspace(a);
+        dims(q, 3); dims(k, 3); dims(v, 3);
+        const int total = narrow_size(q.size(0)), Hq = size(q, 1), D = size(q, 2), Hkv = size(k, 1), R = narrow_size(2 * fr.numel()), dtype = dtype_code(q);
+        require(k.size(0) == total && v.size(0) == total && k.size(2) == D && v.sizes() == k.sizes() && qo.sizes() == q.sizes(), "shapes of Q, K, V and Qout do not match");
+        for (const at::Tensor *t : { &q, &k, &v }) {
+            require(t->is_cuda() && t->scalar_type() == q.scalar_type() && t->device().index() == c10::hip::current_device(), "Q, K and V must be of one type on the current device");
+            require((t->size(2) == 1 || t->stride(2) == 1) && (t->size(1) == 1 || t->stride(1) == D), "heads and channels of Q, K and V must lie side by side");
+        }
+        require(kc.sizes() == vc.sizes() && kc.dim() >= 3 && kc.size(-1) == D && kc.size(-2) == Hkv, "the caches must be [.., Hkv, D]");
+        for (const at::Tensor *t : { &kc, &vc }) {
+            require(t->is_cuda() && t->is_contiguous() && t->device().index() == c10::hip::current_device(), "the caches must be contiguous CUDA tensors on the current device");
+            require(fp8 ? t->element_size() == 1 && q.scalar_type() == at::kBFloat16 : t->scalar_type() == q.scalar_type(),
+                    fp8 ? "one-byte caches and bfloat16 rows" : "the caches must have the rows' type");
+        }
+        const long long num_slots = kc.numel() / ((long long)Hkv * D);
+        const int32_t *position = ints(po, total), *slot = ints(sl, total);
+        const double *inv_freq = typed<double>(fr, at::kDouble, "inv_freq must be a contiguous float64 CUDA tensor");
+        void *out = typed(qo, q.scalar_type(), "Qout must be contiguous and of Q's type");
+        const void *Q = q.data_ptr(), *K = k.data_ptr(), *V = v.data_ptr();
+        void *Kc = kc.data_ptr(), *Vc = vc.data_ptr();
+        const long long qs = q.stride(0), ks = k.stride(0), vs = v.stride(0);
+        return [=](void *st) {
+            return fp8 ? btv_rope_append_fp8kv(Q, qs, K, ks, V, vs, total, Hq, Hkv, D, position, slot, inv_freq, R, interleaved, factor, out, Kc, Vc, k_scale, v_scale,
+                                               num_slots, ws, st)
+                       : btv_rope_append(Q, qs, K, ks, V, vs, dtype, total, Hq, Hkv, D, position, slot, inv_freq, R, interleaved, factor, out, Kc, Vc, num_slots, ws, st);
+        };
+    });
+}
+FACE(rope_append) { return append(args, n, false); }
+FACE(rope_append_fp8kv) { return append(args, n, true); }
+
+PyObject *chunk_attn(PyObject *const *args, Py_ssize_t n, bool fp8)
+{
+    return call(args, n, [fp8](Args &a) {
+        const at::Tensor &q = a.tensor(), &k = a.tensor(), &v = a.tensor();
+        const float k_scale = fp8 ? (float)a.real() : 1.f, v_scale = fp8 ? (float)a.real() : 1.f;
+        const at::Tensor &bt = a.tensor(), &qo = a.tensor(), &pl = a.tensor();
+        const int M_max = a.int32(), L_max = a.int32();
+        const at::Tensor &o = a.tensor();
+        const at::Tensor *w = a.tensor_or_none();
+        const float scale = (float)a.real();
+        dims(q, 3); dims(k, 4); dims(bt, 2);
+        const int total_M = narrow_size(q.size(0)), Hq = size(q, 1), D = size(q, 2), blocks = narrow_size(k.size(0)), Hkv = size(k, 2);
+        const int batch = narrow_size(bt.size(0)), max_blocks = narrow_size(bt.size(1));
+        require(k.size(1) == BTV_PAGE && k.size(3) == D && v.sizes() == k.sizes() && o.sizes() == q.sizes(), "shapes of Q, the pools [blocks, BTV_PAGE, Hkv, D] and O do not match");
+        const void *Q = typed(q, at::kBFloat16, "Q must be a contiguous bfloat16 CUDA tensor");
+        void *O = typed(o, at::kBFloat16, "O must be a contiguous bfloat16 CUDA tensor");
+        if (fp8) require(k.element_size() == 1 && v.element_size() == 1, "K and V must be one byte");
+        const void *K = typed(k, fp8 ? k.scalar_type() : at::kBFloat16, "the pools must be contiguous CUDA tensors, bfloat16 or one byte");
+        const void *V = typed(v, k.scalar_type(), "the pools must be contiguous CUDA tensors of one type");
+        const int32_t *table = ints(bt), *q_offset = ints(qo, (int64_t)batch + 1), *prefix_len = ints(pl, batch);
+        const Workspace ws = { w ? typed(*w, w->scalar_type(), "a workspace is a contiguous CUDA tensor") : nullptr, w ? (size_t)(w->numel() * w->element_size()) : 0 };
+        return [=](void *st) {
+            return fp8 ? btv_chunk_attn_paged_fp8kv(Q, K, V, k_scale, v_scale, blocks, table, max_blocks, q_offset, prefix_len, batch, total_M, M_max, L_max, Hq, Hkv, D,
+                                                    scale, O, ws.ptr, ws.bytes, st)
+                       : btv_chunk_attn_paged(Q, K, V, blocks, table, max_blocks, q_offset, prefix_len, batch, total_M, M_max, L_max, Hq, Hkv, D, scale, O, ws.ptr,
+                                              ws.bytes, st);
+        };
+    });
+}
+FACE(chunk_attn_paged) { return chunk_attn(args, n, false); }
+FACE(chunk_attn_paged_fp8kv) { return chunk_attn(args, n, true); }
+
 PyObject *set_error(PyObject *, PyObject *type)
 {
     Py_INCREF(type);
@@ -415,6 +536,7 @@ PyMethodDef methods[] = {
     ENTRY(tree_build), ENTRY(tree_build_adaptive), ENTRY(tree_build_batch), ENTRY(tree_verify_attn), ENTRY(tree_verify_attn_fp8kv),
     ENTRY(tree_verify_attn_paged), ENTRY(tree_verify_attn_paged_fp8kv), ENTRY(tree_accept_greedy), ENTRY(tree_accept_greedy_batch),
     ENTRY(tree_accept_greedy_lm_head), ENTRY(tree_accept_stochastic), ENTRY(kv_commit), ENTRY(kv_commit_paged),
+    ENTRY(paged_extend), ENTRY(rope_append), ENTRY(rope_append_fp8kv), ENTRY(chunk_attn_paged), ENTRY(chunk_attn_paged_fp8kv),
     { "set_error", set_error, METH_O, nullptr }, { nullptr, nullptr, 0, nullptr },
 };
 PyModuleDef module = { PyModuleDef_HEAD_INIT, "_face", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr };
