@@ -22,6 +22,7 @@ int btv_fail(int code, const char *fmt, ...);   // records the thread-local mess
         if (e_ != hipSuccess) return btv_fail(BTV_EHIP, "%s: %s", #call, hipGetErrorString(e_)); \
     } while (0)
 
+static inline bool btv_aligned16(const void *a) { return (reinterpret_cast<uintptr_t>(a) & 15u) == 0; }
 static inline size_t btv_align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // Workspace layout used by every entry point: word 0 of the workspace is the data-error flag.

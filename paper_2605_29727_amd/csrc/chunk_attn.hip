@@ -1,130 +1,407 @@
-// Causal attention of the requests' new rows over a paged KV cache (gfx950), bf16 or E4M3 K/V.
-#include "btv_common.h"
+// Causal attention of the requests' new rows over a paged KV cache (gfx950), bf16 or E4M3 K/V: prompts, chunks of them and single tokens in one
+// ragged batch.
+//
+// What is computed: row i of request r, which has L rows in the cache ahead of its new ones, sees the keys 0 .. L + i:
+//   O[i,h] = sum_j p_j V[j,g] / sum_j p_j,  p_j = exp2(scale log2(e) (Q[i,h].K[j,g] - m)),  m a reference that follows the largest score.
+// One pass over the keys; rows' sums and accumulators stay in fp32 registers (attn_piece.h).  A workgroup takes a row block of whole nodes (node: a new
+// token; its G = Hq / Hkv query heads are G packed rows, so that a K/V byte serves all of them) and a range of 32-key tiles.  Long chunks are bound
+// by the matrix cores, single tokens by the stream of K/V.
+//
+// The host knows bounds on the lengths only, so the workgroups share the work out themselves.  A row block is START + weight * keys long (the keys that its last node sees;
+// the weight is WHOLE, or PART where no more than half of the block's rows exist and a tile goes faster); blocks lie one after the other, request
+// after request, KV head after KV head, and workgroup k takes what lies between k w and (k + 1) w.  Where that cuts a block, each part's rows go to the
+// workgroup's own place in the workspace (two at most: a block that it carries on with, one that it begins), and chunk_merge joins them in the order of the keys.
+// Neighbouring shares are on one XCD, which so keeps to one KV head or two, whose K/V its workgroups meet in their L2.
+#include "attn_piece.h"
 
-#include <algorithm>
-#include <cfloat>
-#include <cmath>
+#include <atomic>
+#include <climits>
 
 namespace {
 
-constexpr float NEG_BIG = -1.0e30f;
+typedef long long i64;
 
-struct ChunkParams {
-    const void *Q, *K, *V;
-    void *O;
-    const int32_t *block_table, *q_offset, *prefix_len;
-    uint32_t *flag;
-    int batch, total_M, M_max, L_max, Hq, Hkv, G, max_blocks, num_blocks;
-    float scale, out_scale;
+constexpr int WHOLE = 3, PART = 2, START = 10 * 32 * WHOLE;     // lengths in keys times weight
+constexpr int MARGIN = 2, SMALL = 8;                            // tiles: a cut nearer to a block's ends moves there; blocks of up to SMALL are not cut
+constexpr int MOST_ROWS = 1 << 20, MOST_TEAMS = 512;
+
+// What a workgroup leaves for the merge: whether it has begun a block that others carry on with (which one), and whether the block that
+// it carried on with ends with its part.
+struct Left { int flags, rq, g, by; };
+constexpr int BEGUN = 1, ENDED = 2;
+
+struct ChunkParams : AttnParams {
+    Left *left;                   // [teams]
+    int nb;                       // nodes per row block
+    int wr;                       // rows per row block
+    int teams;                    // workgroups: 256 or 512
+    int most_keys;                // what a row of the block table has room for
 };
 
-// A workgroup per (row, query head): 256 keys at a time, scores by one thread per key, values by one thread per channel.
-template <int D, int EB>
-__global__ __launch_bounds__(256) void chunk_attn_simple(ChunkParams p)
+// 64-bit minimum and maximum of numbers less than 2^62 apart, by the sign of their difference.  (Of values that a wavefront has in common the compiler makes a vector
+// comparison and a scalar selection, and has left out what carries the one's result to the other: every share came out as the smallest one.)
+__device__ __forceinline__ i64 least(i64 a, i64 b) { return b + ((a - b) & ((a - b) >> 63)); }
+__device__ __forceinline__ i64 most(i64 a, i64 b) { return a - ((a - b) & ((a - b) >> 63)); }
+
+struct Span { int q0, M, L; bool ok; };
+__device__ __forceinline__ Span load_span(const ChunkParams &p, int r)
 {
-    constexpr int GROUPS = 256 / D, PER = 256 / GROUPS;
-    __shared__ float qs[D], prob[256], red[GROUPS][D], stat[8];
-    __shared__ int mine, pages[16];
-    const int row = blockIdx.x, hq = blockIdx.y, tid = threadIdx.x, g = hq / p.G;
-    if (tid == 0) mine = -1;
-    __syncthreads();
-    for (int r = tid; r < p.batch; r += 256) {
-        const int q0 = p.q_offset[r], q1 = p.q_offset[r + 1], L = p.prefix_len[r];
-        const bool ok = q0 >= 0 && q1 >= q0 && q1 - q0 <= p.M_max && q1 <= p.total_M && L >= 0 && L <= p.L_max && (long long)L + (q1 - q0) <= (long long)p.max_blocks * BTV_PAGE;
-        if (!ok) { if (row == 0 && hq == 0) atomicOr(p.flag, 2u); continue; }
-        if (row >= q0 && row < q1) atomicMax(&mine, r);
-    }
-    __syncthreads();
-    if (mine < 0) return;
-    const int r = mine, L = p.prefix_len[r], S = L + (row - p.q_offset[r]) + 1;
-    const int32_t *bt = p.block_table + (size_t)r * p.max_blocks;
-    if (tid < D) qs[tid] = (float)static_cast<const __bf16 *>(p.Q)[((size_t)row * p.Hq + hq) * D + tid] * p.scale;
-    float m = NEG_BIG, l = 0.f, o = 0.f;
-    const int d = tid % D, kg = tid / D;
-    auto value = [&](const void *pool, int j, int ch) {            // key j of this chunk's 256
-        const size_t at = (((size_t)pages[j >> 4] * BTV_PAGE + (j & 15)) * p.Hkv + g) * D + ch;
-        if constexpr (EB == 1) {
-            const uint32_t c = static_cast<const uint8_t *>(pool)[at];
-            return __builtin_amdgcn_cvt_f32_fp8((int)c, 0);
-        } else {
-            return (float)static_cast<const __bf16 *>(pool)[at];
-        }
-    };
-    for (int j0 = 0; j0 < S; j0 += 256) {
-        __syncthreads();
-        if (tid < 16) pages[tid] = min(max(bt[min((j0 >> 4) + tid, (S - 1) >> 4)], 0), p.num_blocks - 1);
-        __syncthreads();
-        float s = -INFINITY;
-        if (j0 + tid < S) {
-            s = 0.f;
-            for (int ch = 0; ch < D; ++ch) s = fmaf(qs[ch], value(p.K, tid, ch), s);
-        }
-        float mx = s;
-        for (int x = 32; x >= 1; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x));
-        if ((tid & 63) == 0) stat[tid >> 6] = mx;
-        __syncthreads();
-        const float mn = fmaxf(m, fmaxf(fmaxf(stat[0], stat[1]), fmaxf(stat[2], stat[3])));
-        const float pj = j0 + tid < S ? expf(s - mn) : 0.f, alpha = expf(m - mn);
-        m = mn;
-        prob[tid] = pj;
-        float sum = pj;
-        for (int x = 32; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
-        if ((tid & 63) == 0) stat[4 + (tid >> 6)] = sum;
-        __syncthreads();
-        l = l * alpha + stat[4] + stat[5] + stat[6] + stat[7];
-        o *= alpha;
-        for (int j = kg * PER; j < min(kg * PER + PER, S - j0); ++j) o = fmaf(prob[j], value(p.V, j, d), o);
-    }
-    red[kg][d] = o;
-    __syncthreads();
-    if (tid < D) {
-        float x = red[0][tid];
-        for (int k = 1; k < GROUPS; ++k) x += red[k][tid];
-        static_cast<__bf16 *>(p.O)[((size_t)row * p.Hq + hq) * D + tid] = (__bf16)(x / l * p.out_scale);
-    }
+    Span s;
+    const int q1 = p.q_offset[r + 1];
+    s.q0 = p.q_offset[r];
+    s.L = p.prefix_len[r];
+    s.ok = s.q0 >= 0 && q1 >= s.q0 && q1 <= p.total_M && s.L >= 0 && s.L <= p.L;
+    s.M = s.ok ? q1 - s.q0 : 0;
+    if (s.M > p.M || (s.ok && s.L + s.M > p.most_keys)) { s.ok = false; s.M = 0; }
+    return s;
 }
 
-constexpr int MOST_ROWS = 1 << 20;
+__device__ __forceinline__ int part_weight(const ChunkParams &p, int nodes) { return nodes * p.G * 2 <= p.wr ? PART : WHOLE; }
+// Length of a request's first b blocks (whole ones)
+__device__ __forceinline__ i64 length_to(const ChunkParams &p, int L, i64 b) { return b * (START + (i64)WHOLE * L) + (i64)WHOLE * p.nb * (b * (b + 1) / 2); }
+__device__ __forceinline__ i64 length_of(const ChunkParams &p, int L, int M)
+{
+    const int whole = M / p.nb, rest = M - whole * p.nb;
+    return length_to(p, L, whole) + (rest ? START + (i64)part_weight(p, rest) * (L + M) : 0);
+}
+
+__device__ __forceinline__ i64 wave_incl_scan(i64 x, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const i64 y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
+}
+__device__ __forceinline__ i64 lane_value(i64 x, int lane)
+{
+    return (i64)(((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)x, lane));
+}
+
+// 64 requests, one per lane, and where each ends in a KV head's work.
+struct Chunk { int L, M; i64 incl; bool bad; };
+__device__ __forceinline__ Chunk load_chunk(const ChunkParams &p, int c0, int lane, i64 before)
+{
+    Chunk c = {};
+    if (c0 + lane < p.batch) {
+        const Span s = load_span(p, c0 + lane);
+        c.L = s.L; c.M = s.M; c.bad = !s.ok;
+    }
+    c.incl = wave_incl_scan(c.M ? length_of(p, c.L, c.M) : 0, lane) + before;
+    return c;
+}
+// The first chunk is kept in LDS from one piece to the next (raw instructions: ahead of ordinary reads the compiler waits for the last piece's stores), but where
+// two workgroups fill the LDS of a CU to the last byte; there it is loaded again.
+constexpr int CHUNK_BYTES = 64 * 16;
+template <int D, int RW, int KW, int NT, int EB>
+struct ChunkLds {
+    using PL = PageLds<D, RW, KW, NT, true, EB>;
+    static constexpr bool KEPT = (PL::BYTES + CHUNK_BYTES) * PL::PER_CU <= 160 * 1024;
+    static constexpr int BYTES = PL::BYTES + (KEPT ? CHUNK_BYTES : 0);
+};
+__device__ __forceinline__ void keep_chunk(uint32_t kept, int lane, const Chunk &c)
+{
+    const u32x4 a = { (uint32_t)c.L, (uint32_t)c.M, (uint32_t)c.incl, (uint32_t)(c.incl >> 32) };
+    asm volatile("ds_write_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" :: "v"(kept + (uint32_t)lane * 16), "v"(a) : "memory");
+}
+__device__ __forceinline__ Chunk kept_chunk(uint32_t kept, int lane)
+{
+    u32x4 a;
+    asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(a) : "v"(kept + (uint32_t)lane * 16) : "memory");
+    Chunk c;
+    c.L = (int)a[0]; c.M = (int)a[1]; c.incl = (i64)((unsigned long long)a[3] << 32 | a[2]); c.bad = false;
+    return c;
+}
+
+// Where a workgroup stands (every wavefront works it out for itself).
+struct Walk {
+    i64 pos, end;                 // its share, and what comes next
+    i64 head, wh;                 // where the current KV head's work begins; one head's work
+    int h, team;                  // that head; the workgroup's place in the order of the shares
+};
+
+__device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool leader, Chunk &c)
+{
+    Walk k;
+    i64 all = 0;
+    bool bad = false;
+    for (int c0 = ((p.batch - 1) >> 6) << 6; c0 >= 0; c0 -= 64) {       // (the first chunk last; where the others end does not matter yet)
+        c = load_chunk(p, c0, lane, 0);
+        bad = bad || c.bad;
+        all += lane_value(c.incl, 63);
+    }
+    if (leader && bad) atomicOr(p.flag, 2u);
+    k.wh = all;
+    all *= p.Hkv;
+    const int teams_log2 = 31 - __builtin_clz(p.teams);
+    const i64 w = most((all + p.teams - 1) >> teams_log2, p.wmin);
+    // as many shares on each XCD: where the work is for a part of the workgroups, all XCDs have some
+    const int xcd = blockIdx.x & 7, nth = blockIdx.x >> 3;
+    int per_xcd = p.teams >> 3;
+    if (w == p.wmin) per_xcd = min(per_xcd, (((int)all + p.wmin - 1) / p.wmin + 7) >> 3);       // (all is teams * wmin at most)
+    if (nth < per_xcd) {
+        k.team = xcd * per_xcd + nth;
+        k.pos = least(k.team * w, all);
+        k.end = least(k.pos + w, all);
+    } else {
+        k.team = 8 * per_xcd + (nth - per_xcd) * 8 + xcd;               // (the others have no work, but say so)
+        k.pos = k.end = all;
+    }
+    k.head = 0; k.h = 0;
+    return k;
+}
+
+// The next piece; the walk moves behind it.  False: none left.  c holds the first chunk of requests.
+__device__ __forceinline__ bool next_piece(const ChunkParams &p, Walk &k, int lane, const Chunk &c, Piece &pc, Left &left)
+{
+    while (k.pos < k.end) {
+        while (k.pos - k.head >= k.wh) { k.head += k.wh; ++k.h; }
+        const i64 x = k.pos - k.head;
+        Chunk d = c;
+        int r0 = 0;
+        unsigned long long beyond;
+        while ((beyond = __builtin_amdgcn_ballot_w64(x < d.incl)) == 0ull) {
+            r0 += 64;
+            if (r0 >= p.batch) return false;            // (cannot be: x lies within the head's work)
+            d = load_chunk(p, r0, lane, lane_value(d.incl, 63));
+        }
+        const int src = __builtin_ctzll(beyond);
+        const int L = __builtin_amdgcn_readlane(d.L, src), M = __builtin_amdgcn_readlane(d.M, src);
+        const i64 y = x - (lane_value(d.incl, src) - length_of(p, L, M));              // place in the request's work
+        const int whole = M / p.nb;
+        // the block: the largest b with length_to(b) <= y, from the quadratic's root
+        const double q1 = START + (double)WHOLE * L + 0.5 * WHOLE * p.nb, q2 = 0.5 * WHOLE * p.nb;
+        int b = __builtin_amdgcn_readfirstlane((int)fmin((sqrt(q1 * q1 + 4.0 * q2 * (double)y) - q1) / (2.0 * q2), (double)whole));
+        while (b > 0 && length_to(p, L, b) > y) --b;
+        while (b < whole && length_to(p, L, b + 1) <= y) ++b;
+        const int node0 = b * p.nb, nodes = min(p.nb, M - node0), keys = L + node0 + nodes, t = (keys + 31) >> 5;
+        const int wt = b < whole ? WHOLE : part_weight(p, nodes);
+        const int y0 = (int)(y - length_to(p, L, b)), cl = wt * keys, cm = MARGIN * 32 * wt;
+        const i64 us = k.pos - y0;
+        pc.rq = r0 + src; pc.g = k.h; pc.by = b; pc.node0 = node0; pc.nodes = nodes;
+        pc.bx = 0; pc.st0 = 0; pc.st1 = t; pc.direct = 1;
+        if (t <= SMALL) {                               // to the share in which it begins
+            k.pos = us + START + cl;
+            if (y0 == 0) return true;
+            continue;
+        }
+        const i64 ts = us + START;
+        int c0 = y0 - START, c1 = (int)least(k.end - ts, cl);
+        c0 = c0 < cm ? 0 : c0 > cl - cm ? cl : c0;
+        c1 = c1 < cm ? 0 : c1 > cl - cm ? cl : c1;
+        k.pos = c1 < cl ? k.end : ts + cl;
+        if (c0 >= c1) continue;
+        pc.st0 = c0 / 32 / wt;
+        pc.st1 = c1 == cl ? t : c1 / 32 / wt;
+        const bool first = c0 == 0, last = c1 == cl;
+        pc.direct = first && last;
+        pc.prow0 = (2 * k.team + (first ? 1 : 0)) * p.wr;
+        if (first && !last) { left.flags |= BEGUN; left.rq = pc.rq; left.g = pc.g; left.by = b; }
+        if (!first && last) left.flags |= ENDED;
+        return true;
+    }
+    return false;
+}
+
+template <int D, int RW, int KW, int NT, int EB>
+__global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams p)
+{
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    // (every argument in one round trip)
+    asm volatile("" ::"s"(p.Q), "s"(p.K), "s"(p.V), "s"(p.O), "s"(p.block_table), "s"(p.q_offset), "s"(p.prefix_len), "s"(p.Opart), "s"(p.ML), "s"(p.flag), "s"(p.M),
+                 "s"(p.L), "s"(p.Hq), "s"(p.Hkv), "s"(p.G), "s"(p.ginv), "s"(p.max_blocks), "s"(p.num_blocks), "s"(p.total_M), "s"(p.batch), "s"(p.wmin),
+                 "s"(p.scale_log2), "s"(p.out_scale), "s"(p.left), "s"(p.nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys));
+    Chunk c;
+    Walk k = share_out(p, threadIdx.x & 63, blockIdx.x == 0 && threadIdx.x < 64, c);
+    using CL = ChunkLds<D, RW, KW, NT, EB>;
+    const uint32_t kept = (uint32_t)(uintptr_t)BTV_LDS_PTR(smem) + CL::PL::BYTES;
+    if (CL::KEPT && threadIdx.x < 64) keep_chunk(kept, threadIdx.x, c);     // (barriers before it is read: those of the first piece)
+    Left left = { 0, 0, 0, 0 };
+    for (bool again = false;; again = true) {
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));                   // keeps what derives from it (all addresses) from being carried across pieces
+        if (again) {
+            if (k.pos >= k.end) break;
+            c = CL::KEPT ? kept_chunk(kept, tid & 63) : load_chunk(p, 0, tid & 63, 0);
+        }
+        Piece pc = {};
+        if (!next_piece(p, k, tid & 63, c, pc, left)) break;
+        const Span s = load_span(p, pc.rq);
+        const Req rq = { s.q0, s.M, s.L, true };
+        attn_piece<D, RW, KW, NT, true, EB, true>(p, smem, tid, rq, pc, [] {});
+        // every wave is done with this piece's LDS, its own fills have landed; the stores may still be on their way
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+    }
+    if (threadIdx.x == 0) p.left[k.team] = left;
+}
+
+// The blocks that were cut: 16 lanes per row, 16 rows per workgroup; workgroup (k, slice) looks at the block that share k has begun.  Parts are added in the order of
+// their keys, each relative to the row's largest reference; they come in fp16 beside their magnitude (attn_piece.h), sums are fp32.
+template <int D>
+__global__ __launch_bounds__(256) void chunk_merge(ChunkParams p)
+{
+    constexpr int E = D / 16;
+    typedef _Float16 hvec __attribute__((ext_vector_type(E)));
+    typedef __bf16 bvec __attribute__((ext_vector_type(E)));
+    const int k = blockIdx.x, lane = threadIdx.x & 63;
+    const Left left = p.left[k];
+    if (!(left.flags & BEGUN)) return;
+    // the first share behind k that ends a block ends this one (those between lie within it)
+    int n = 0;
+    for (int k0 = k + 1;; k0 += 64) {
+        const int at = k0 + lane;
+        const unsigned long long ended = __builtin_amdgcn_ballot_w64(at >= p.teams || (p.left[min(at, p.teams - 1)].flags & ENDED));
+        if (ended) { n = k0 - k + __builtin_ctzll(ended) + 1; break; }
+    }
+    if (k + n > p.teams) return;                        // (cannot be)
+    const Span s = load_span(p, left.rq);
+    const int node0 = left.by * p.nb, nodes = min(p.nb, s.M - node0), x = blockIdx.y * 16 + (threadIdx.x >> 4), node = (x * p.ginv) >> 16;
+    if (node >= nodes) return;
+    const int sub = threadIdx.x & 15;
+    auto row_of = [&](int i) { return (size_t)(2 * (k + i) + (i == 0)) * p.wr + x; };
+    float mmax = NEG_BIG;
+    for (int i = sub; i < n; i += 16) mmax = fmaxf(mmax, p.ML[row_of(i) * 4]);
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) mmax = fmaxf(mmax, __shfl_xor(mmax, d));
+    float acc[E], den = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    for (int i0 = 0; i0 < n; i0 += 4) {
+        hvec part[4];
+        float4 ml[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const size_t row = row_of(min(i0 + b, n - 1));
+            ml[b] = *reinterpret_cast<const float4 *>(p.ML + row * 4);
+            part[b] = *reinterpret_cast<const hvec *>(p.Opart + row * D + sub * E);
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const float w = i0 + b < n ? __builtin_amdgcn_exp2f(ml[b].x - mmax) : 0.f;
+            den += w * ml[b].y;
+            const float wa = w * ml[b].z;
+            if (wa != 0.f)                              // (a part that the row sees none of has nothing to add)
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = fmaf(wa, (float)part[b][e], acc[e]);
+        }
+    }
+    const float inv = p.out_scale / den;
+    bvec o;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = (__bf16)(acc[e] * inv);
+    const size_t orow = (size_t)(s.q0 + node0 + node) * p.Hq + left.g * p.G + (x - node * p.G);
+    *reinterpret_cast<bvec *>(static_cast<__bf16 *>(p.O) + orow * D + sub * E) = o;
+}
+
+// ---- host side ------------------------------------------------------------------------------------------------------------
 
 int check_chunk(int batch, int M_max, int L_max, int Hq, int Hkv, int D)
 {
     BTV_REQUIRE(batch >= 1 && batch <= 4096, "batch=%d outside [1,4096]", batch);
     BTV_REQUIRE(M_max >= 1 && M_max <= MOST_ROWS, "M_max=%d outside [1,%d]", M_max, MOST_ROWS);
-    BTV_REQUIRE(L_max >= 0 && (long long)L_max + M_max < (1ll << 30), "L_max=%d out of range", L_max);
+    BTV_REQUIRE(L_max >= 0 && (i64)L_max + M_max < (1ll << 29), "L_max=%d out of range", L_max);         // (weighted lengths of a block stay in 32 bits)
     BTV_REQUIRE(Hq >= 1 && Hkv >= 1 && Hkv <= 1024 && Hq % Hkv == 0 && Hq / Hkv <= 16, "bad heads Hq=%d Hkv=%d", Hq, Hkv);
     BTV_REQUIRE(D == 64 || D == 128, "D=%d not in {64,128}", D);
+    // the work's length stays in 62 bits: per request and head at most M/4 + 1 blocks
+    const double block = START + (double)WHOLE * ((double)L_max + M_max);
+    BTV_REQUIRE((double)batch * Hkv * (M_max / 4 + 1) * block < 4.0e18, "more work than can be counted");
     return BTV_OK;
 }
 
-bool aligned16(const void *a) { return (reinterpret_cast<uintptr_t>(a) & 15u) == 0; }
+// Rows per workgroup by the largest request's packed rows.
+int rows_per_block(int M_max, int G, int eb)
+{
+    const i64 rows = (i64)M_max * G;
+    return rows <= 64 ? 64 : rows <= 128 || eb == 1 ? 128 : 256;
+}
+int teams_of(int wr) { return wr == 64 ? 512 : 256; }           // one workgroup per CU, or two of the small ones
+bool cuts(int M_max, int L_max) { return (L_max + M_max + 31) / 32 > SMALL; }
+
+struct WsLayout { size_t left, ml, opart, total; };
+WsLayout ws_layout(int wr, int D, bool cut)
+{
+    WsLayout w;
+    size_t off = BTV_WS_HEADER + MERGE_WORDS;
+    const size_t rows = cut ? (size_t)teams_of(wr) * 2 * wr : 0;
+    w.left = off; off += MOST_TEAMS * sizeof(Left);
+    w.ml = off; off += rows * 16;
+    w.opart = off; off += rows * D * 2;
+    w.total = btv_align_up(off, BTV_WS_ALIGN);
+    return w;
+}
+size_t enough_for(int M_max, int L_max, int G, int D, int eb)
+{
+    const bool cut = cuts(M_max, L_max);
+    size_t most = 0;
+    for (int wr = 64; wr <= rows_per_block(M_max, G, eb); wr *= 2) most = std::max(most, ws_layout(wr, D, cut).total);
+    return most;
+}
+
+template <int D, int RW, int KW, int NT, int EB>
+int launch(const ChunkParams &p, hipStream_t st)
+{
+    constexpr int LDS_BYTES = ChunkLds<D, RW, KW, NT, EB>::BYTES;
+    static_assert(LDS_BYTES * (RW * KW <= 4 ? 2 : 1) <= 160 * 1024, "LDS budget");
+    static std::atomic<unsigned long long> configured{0};       // a bit per device
+    int dev = 0;
+    BTV_HIP(hipGetDevice(&dev));
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (!(configured.load(std::memory_order_acquire) & bit)) {
+        BTV_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(chunk_attn_kernel<D, RW, KW, NT, EB>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES));
+        configured.fetch_or(bit, std::memory_order_release);
+    }
+    hipLaunchKernelGGL((chunk_attn_kernel<D, RW, KW, NT, EB>), dim3(p.teams), dim3(RW * KW * 64), LDS_BYTES, st, p);
+    BTV_HIP(hipGetLastError());
+    return BTV_OK;
+}
 
 int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_blocks, const int32_t *block_table, int max_blocks, const int32_t *q_offset,
                const int32_t *prefix_len, int batch, int total_M, int M_max, int L_max, int Hq, int Hkv, int D, int eb, float scale, float k_scale,
                float v_scale, void *O, void *ws, size_t ws_bytes, void *stream)
 {
     BTV_REQUIRE(((Q && O) || total_M == 0) && Kpool && Vpool && block_table && q_offset && prefix_len, "null pointer");
-    BTV_REQUIRE(aligned16(Q) && aligned16(Kpool) && aligned16(Vpool) && aligned16(O), "Q, K, V and O must be 16-byte aligned");
+    BTV_REQUIRE(btv_aligned16(Q) && btv_aligned16(Kpool) && btv_aligned16(Vpool) && btv_aligned16(O), "Q, K, V and O must be 16-byte aligned");
     int rc = check_chunk(batch, M_max, L_max, Hq, Hkv, D);
     if (rc) return rc;
-    BTV_REQUIRE(total_M >= 0 && total_M <= INT32_MAX / Hq, "total_M=%d out of range", total_M);
+    BTV_REQUIRE(total_M >= 0 && total_M <= INT_MAX / Hq, "total_M=%d out of range", total_M);
     BTV_REQUIRE(num_blocks >= 1 && max_blocks >= 1, "bad block counts");
-    BTV_REQUIRE((long long)max_blocks * BTV_PAGE >= (long long)L_max + 1, "max_blocks too small for L_max");
+    BTV_REQUIRE((i64)max_blocks * BTV_PAGE >= (i64)L_max + 1, "max_blocks too small for L_max");
     BTV_REQUIRE(std::isfinite(scale) && std::fabs(scale) <= 1e30f, "the scale must be finite");
-    rc = btv_check_ws(ws, ws_bytes, BTV_WS_HEADER);
+    const float factor = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) * k_scale * 1.4426950408889634f;
+    BTV_REQUIRE(std::isfinite(factor) && factor > 0.f, "the scale must be finite");
+    const int G = Hq / Hkv, wr = rows_per_block(M_max, G, eb);
+    const bool cut = cuts(M_max, L_max);
+    const WsLayout wl = ws_layout(wr, D, cut);
+    rc = btv_check_ws(ws, ws_bytes, wl.total);
     if (rc) return rc;
     if (total_M == 0) return BTV_OK;
+    unsigned char *w8 = static_cast<unsigned char *>(ws);
     ChunkParams p = {};
-    p.Q = Q; p.K = Kpool; p.V = Vpool; p.O = O; p.block_table = block_table; p.q_offset = q_offset; p.prefix_len = prefix_len;
-    p.flag = static_cast<uint32_t *>(ws);
-    p.batch = batch; p.total_M = total_M; p.M_max = M_max; p.L_max = L_max; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv;
-    p.max_blocks = max_blocks; p.num_blocks = num_blocks;
-    p.scale = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) * k_scale;
-    p.out_scale = v_scale;
-    const dim3 grid(total_M, Hq);
+    p.Q = Q; p.K = Kpool; p.V = Vpool; p.O = O;
+    p.block_table = block_table; p.q_offset = q_offset; p.prefix_len = prefix_len;
+    p.Opart = reinterpret_cast<_Float16 *>(w8 + wl.opart);
+    p.ML = reinterpret_cast<float *>(w8 + wl.ml);
+    p.flag = reinterpret_cast<uint32_t *>(w8);
+    p.M = M_max; p.L = L_max; p.Hq = Hq; p.Hkv = Hkv; p.G = G; p.ginv = (65536 + G - 1) / G;
+    p.max_blocks = max_blocks; p.num_blocks = num_blocks; p.total_M = total_M; p.batch = batch;
+    p.scale_log2 = factor; p.out_scale = v_scale;
+    p.left = reinterpret_cast<Left *>(w8 + wl.left);
+    p.wr = wr; p.nb = wr / G; p.teams = teams_of(wr);
+    p.wmin = 2 * START;
+    p.most_keys = (int)std::min<i64>((i64)max_blocks * BTV_PAGE, INT_MAX);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (eb == 1) hipLaunchKernelGGL((chunk_attn_simple<128, 1>), grid, dim3(256), 0, st, p);
-    else if (D == 64) hipLaunchKernelGGL((chunk_attn_simple<64, 2>), grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL((chunk_attn_simple<128, 2>), grid, dim3(256), 0, st, p);
+#define BTV_CASE(DD, EE, RR, KK, NN) if (D == DD && eb == EE && wr == RR * 32) rc = launch<DD, RR, KK, NN, EE>(p, st); else
+    BTV_CASE(128, 2, 2, 2, 5) BTV_CASE(128, 2, 4, 2, 8) BTV_CASE(128, 2, 8, 1, 8)
+    BTV_CASE(64, 2, 2, 2, 5) BTV_CASE(64, 2, 4, 2, 8) BTV_CASE(64, 2, 8, 1, 8)
+    BTV_CASE(128, 1, 2, 2, 5) BTV_CASE(128, 1, 4, 2, 8)
+    return btv_fail(BTV_EINVAL, "no kernel for D=%d", D);
+#undef BTV_CASE
+    if (rc || !cut) return rc;
+    const dim3 grid(p.teams, wr / 16);
+    if (D == 64) hipLaunchKernelGGL(chunk_merge<64>, grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL(chunk_merge<128>, grid, dim3(256), 0, st, p);
     BTV_HIP(hipGetLastError());
     return BTV_OK;
 }
@@ -135,7 +412,7 @@ extern "C" {
 
 size_t btv_chunk_attn_paged_workspace(int batch, int M_max, int L_max, int Hq, int Hkv, int D)
 {
-    return check_chunk(batch, M_max, L_max, Hq, Hkv, D) == BTV_OK ? BTV_WS_HEADER : 0;
+    return check_chunk(batch, M_max, L_max, Hq, Hkv, D) == BTV_OK ? enough_for(M_max, L_max, Hq / Hkv, D, 2) : 0;
 }
 
 int btv_chunk_attn_paged(const void *Q, const void *Kpool, const void *Vpool, int num_blocks, const int32_t *block_table, int max_blocks,
@@ -148,7 +425,7 @@ int btv_chunk_attn_paged(const void *Q, const void *Kpool, const void *Vpool, in
 
 size_t btv_chunk_attn_paged_fp8kv_workspace(int batch, int M_max, int L_max, int Hq, int Hkv, int D)
 {
-    return check_chunk(batch, M_max, L_max, Hq, Hkv, D) == BTV_OK && D == 128 ? BTV_WS_HEADER : 0;
+    return check_chunk(batch, M_max, L_max, Hq, Hkv, D) == BTV_OK && D == 128 ? enough_for(M_max, L_max, Hq / Hkv, D, 1) : 0;
 }
 
 int btv_chunk_attn_paged_fp8kv(const void *Q, const void *K8pool, const void *V8pool, float k_scale, float v_scale, int num_blocks,

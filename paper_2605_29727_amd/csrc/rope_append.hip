@@ -77,8 +77,6 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeParams p)
     }
 }
 
-bool aligned16(const void *a) { return (reinterpret_cast<uintptr_t>(a) & 15u) == 0; }
-
 int rope_append(RopeParams p, int dtype, int eb, int D, void *stream)
 {
     BTV_REQUIRE(dtype == BTV_F32 || dtype == BTV_BF16, "dtype=%d unsupported", dtype);
@@ -92,7 +90,7 @@ int rope_append(RopeParams p, int dtype, int eb, int D, void *stream)
     if (p.total == 0) return BTV_OK;
     BTV_REQUIRE(p.Q && p.K && p.V && p.position && p.slot && p.Qout && p.Kc && p.Vc && (p.inv_freq || p.R == 0), "null pointer");
     const int per16 = dtype == BTV_F32 ? 4 : 8;
-    BTV_REQUIRE(aligned16(p.Q) && aligned16(p.K) && aligned16(p.V) && aligned16(p.Qout) && aligned16(p.Kc) && aligned16(p.Vc),
+    BTV_REQUIRE(btv_aligned16(p.Q) && btv_aligned16(p.K) && btv_aligned16(p.V) && btv_aligned16(p.Qout) && btv_aligned16(p.Kc) && btv_aligned16(p.Vc),
                 "Q, K, V, Qout and the caches must be 16-byte aligned");
     BTV_REQUIRE((reinterpret_cast<uintptr_t>(p.inv_freq) & 7u) == 0, "inv_freq must be 8-byte aligned");
     BTV_REQUIRE(p.q_stride % per16 == 0 && p.k_stride % per16 == 0 && p.v_stride % per16 == 0, "rows must be multiples of 16 bytes apart");

@@ -114,6 +114,14 @@ def test_one_request(kv, Hq, Hkv, D, Ls, Ms):
     check(b, run(b))
 
 
+@pytest.mark.parametrize("kv,Hq,Hkv,D", [("bf16", 32, 8, 128), ("bf16", 32, 8, 64), ("fp8", 32, 8, 128), ("bf16", 28, 4, 128)], ids=["bf16_d128", "bf16_d64", "fp8", "bf16_7_heads"])
+@pytest.mark.parametrize("Ls,Ms", [([8192], [300]), ([0], [2048]), ([4099], [2047]), ([100, 6000, 0, 2222], [900, 1, 1500, 63]), ([30000] * 3, [1] * 3), ([12000], [60])],
+                         ids=lambda x: "-".join(map(str, x)))
+def test_work_for_all_workgroups(kv, Hq, Hkv, D, Ls, Ms):
+    b = make(sum(Ls) + 7 * sum(Ms), Ls, Ms, Hq, Hkv, D, kv)
+    check(b, run(b))
+
+
 @pytest.mark.parametrize("kv,Hq,Hkv,D", SHAPES, ids=SHAPE_IDS)
 @pytest.mark.parametrize("Ls,Ms", [([10, 0, 700, 33], [1, 1, 1, 1]), ([0, 100, 50], [40, 0, 7]), ([0, 4000, 17, 900], [500, 1, 64, 130]), ([0, 0, 0], [300, 1, 77]),
                                    ([7, 12000, 3], [0, 3, 0]), ([40, 6000, 1, 300, 2000], [33, 1, 257, 16, 65])], ids=lambda x: "-".join(map(str, x)))
@@ -177,9 +185,13 @@ def test_nan_in_hidden_places(kv, L, M, at):
             sees = torch.zeros(M + 20, dtype=torch.bool, device="cuda")
             sees[max(at - L, 0):M] = True
             assert torch.equal(O[~sees], clean[~sees]) and torch.equal(O[sees][:, :4], clean[sees][:, :4])
-            hit = O[sees][:, 4:]
+            hit, was = O[sees][:, 4:].double(), clean[sees][:, 4:].double()
             if what == "V":
-                assert bool((~torch.isfinite(hit[..., 77])).all()) and torch.equal(hit[..., :77], clean[sees][:, 4:, :77])
+                # The other channels of a row in several parts may move: a part travels in fp16 beside its largest magnitude, which that channel no longer takes part in, so
+                # both results are off by a half step 2^-11 of the row's parts (of up to twice its largest number), and then by a half step 2^-8 of their own.
+                other = torch.arange(128, device="cuda") != 77
+                limit = 2 * (2.0 ** -10 * was.abs().amax(-1, keepdim=True) * 2 + 2.0 ** -8 * was.abs())
+                assert bool((~torch.isfinite(hit[..., 77])).all()) and bool(((hit - was).abs() <= limit)[..., other].all())
             else:
                 assert bool(torch.isnan(hit).all())
 
