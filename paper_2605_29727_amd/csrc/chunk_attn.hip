@@ -21,21 +21,25 @@ namespace {
 
 typedef long long i64;
 
-constexpr int WHOLE = 3, PART = 2, START = 10 * 32 * WHOLE;     // lengths in keys times weight
+constexpr int WHOLE = 3, PART = 2;                              // weights of a key
 constexpr int MARGIN = 2, SMALL = 8;                            // tiles: a cut nearer to a block's ends moves there; blocks of up to SMALL are not cut
+constexpr int LEAST_PART = 4;                                   // tiles of the smallest part of a token's keys
 constexpr int MOST_ROWS = 1 << 20, MOST_TEAMS = 512;
 
-// What a workgroup leaves for the merge: whether it has begun a block that others carry on with (which one), and whether the block that
-// it carried on with ends with its part.
-struct Left { int flags, rq, g, by; };
+// What a workgroup leaves for the merge: whether it has begun a block that others carry on with (and where that one's rows are), and whether the block
+// that it carried on with ends with its part.
+struct Left { int flags, row0, nodes, g; };                     // row0: the block's first row of Q and O as [total_M]
 constexpr int BEGUN = 1, ENDED = 2;
 
 struct ChunkParams : AttnParams {
     Left *left;                   // [teams]
     int nb;                       // nodes per row block
+    uint32_t inv_nb;              // for quotient()
     int wr;                       // rows per row block
     int teams;                    // workgroups: 256 or 512
+    int start;                    // what a row block costs besides its keys
     int most_keys;                // what a row of the block table has room for
+    int parts;                    // whether every request is one row block, and all of them and their parts may have workgroups of their own
 };
 
 // 64-bit minimum and maximum of numbers less than 2^62 apart, by the sign of their difference.  (Of values that a wavefront has in common the compiler makes a vector
@@ -43,36 +47,33 @@ struct ChunkParams : AttnParams {
 __device__ __forceinline__ i64 least(i64 a, i64 b) { return b + ((a - b) & ((a - b) >> 63)); }
 __device__ __forceinline__ i64 most(i64 a, i64 b) { return a - ((a - b) & ((a - b) >> 63)); }
 
-struct Span { int q0, M, L; bool ok; };
-__device__ __forceinline__ Span load_span(const ChunkParams &p, int r)
-{
-    Span s;
-    const int q1 = p.q_offset[r + 1];
-    s.q0 = p.q_offset[r];
-    s.L = p.prefix_len[r];
-    s.ok = s.q0 >= 0 && q1 >= s.q0 && q1 <= p.total_M && s.L >= 0 && s.L <= p.L;
-    s.M = s.ok ? q1 - s.q0 : 0;
-    if (s.M > p.M || (s.ok && s.L + s.M > p.most_keys)) { s.ok = false; s.M = 0; }
-    return s;
-}
-
 __device__ __forceinline__ int part_weight(const ChunkParams &p, int nodes) { return nodes * p.G * 2 <= p.wr ? PART : WHOLE; }
 // Length of a request's first b blocks (whole ones)
-__device__ __forceinline__ i64 length_to(const ChunkParams &p, int L, i64 b) { return b * (START + (i64)WHOLE * L) + (i64)WHOLE * p.nb * (b * (b + 1) / 2); }
+__device__ __forceinline__ i64 length_to(const ChunkParams &p, int L, int b)
+{
+    return b * (p.start + (i64)WHOLE * L) + (i64)(WHOLE * p.nb) * (i64)((unsigned long long)((i64)b * (b + 1)) >> 1);
+}
 __device__ __forceinline__ i64 length_of(const ChunkParams &p, int L, int M)
 {
-    const int whole = M / p.nb, rest = M - whole * p.nb;
-    return length_to(p, L, whole) + (rest ? START + (i64)part_weight(p, rest) * (L + M) : 0);
+    const int whole = quotient(M, p.nb, p.inv_nb), rest = M - whole * p.nb;
+    return length_to(p, L, whole) + (rest ? p.start + (i64)part_weight(p, rest) * (L + M) : 0);
 }
 
-__device__ __forceinline__ i64 wave_incl_scan(i64 x, int lane)
+// Inclusive sums over the lanes, of numbers below 2^26; of lengths below 2^54 in three pieces.
+__device__ __forceinline__ int wave_sums(int x)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const i64 y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+    // (rows of 16 by shifts, then the last lane of each row into the rows behind it)
+#define BTV_SCAN_STEP(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xF, ctrl < 0x142)
+    BTV_SCAN_STEP(0x111, 0xF); BTV_SCAN_STEP(0x112, 0xF); BTV_SCAN_STEP(0x114, 0xF); BTV_SCAN_STEP(0x118, 0xF);
+    BTV_SCAN_STEP(0x142, 0xA); BTV_SCAN_STEP(0x143, 0xC);
+#undef BTV_SCAN_STEP
     return x;
+}
+__device__ __forceinline__ i64 wave_sums_of_lengths(i64 x)
+{
+    constexpr int B = 18;
+    const i64 lo = wave_sums((int)x & ((1 << B) - 1)), mid = wave_sums((int)(x >> B) & ((1 << B) - 1)), hi = wave_sums((int)(x >> 2 * B));
+    return lo + (mid << B) + (hi << 2 * B);
 }
 __device__ __forceinline__ i64 lane_value(i64 x, int lane)
 {
@@ -80,20 +81,26 @@ __device__ __forceinline__ i64 lane_value(i64 x, int lane)
 }
 
 // 64 requests, one per lane, and where each ends in a KV head's work.
-struct Chunk { int L, M; i64 incl; bool bad; };
+struct Chunk { int q0, L, M; i64 incl; bool bad; };
 __device__ __forceinline__ Chunk load_chunk(const ChunkParams &p, int c0, int lane, i64 before)
 {
-    Chunk c = {};
-    if (c0 + lane < p.batch) {
-        const Span s = load_span(p, c0 + lane);
-        c.L = s.L; c.M = s.M; c.bad = !s.ok;
-    }
-    c.incl = wave_incl_scan(c.M ? length_of(p, c.L, c.M) : 0, lane) + before;
+    Chunk c;
+    const bool in = c0 + lane < p.batch;
+    const int r = min(c0 + lane, p.batch - 1);
+    const int q1 = p.q_offset[r + 1];
+    c.q0 = p.q_offset[r];
+    c.L = p.prefix_len[r];
+    bool ok = c.q0 >= 0 && q1 >= c.q0 && q1 <= p.total_M && c.L >= 0 && c.L <= p.L;
+    c.M = ok ? q1 - c.q0 : 0;
+    ok = ok && c.M <= p.M && c.L + c.M <= p.most_keys;
+    c.bad = in && !ok;
+    if (!in || !ok) c.M = c.L = 0;
+    c.incl = wave_sums_of_lengths(c.M ? length_of(p, c.L, c.M) : 0) + before;
     return c;
 }
 // The first chunk is kept in LDS from one piece to the next (raw instructions: ahead of ordinary reads the compiler waits for the last piece's stores), but where
 // two workgroups fill the LDS of a CU to the last byte; there it is loaded again.
-constexpr int CHUNK_BYTES = 64 * 16;
+constexpr int CHUNK_BYTES = 64 * 32;
 template <int D, int RW, int KW, int NT, int EB>
 struct ChunkLds {
     using PL = PageLds<D, RW, KW, NT, true, EB>;
@@ -102,15 +109,15 @@ struct ChunkLds {
 };
 __device__ __forceinline__ void keep_chunk(uint32_t kept, int lane, const Chunk &c)
 {
-    const u32x4 a = { (uint32_t)c.L, (uint32_t)c.M, (uint32_t)c.incl, (uint32_t)(c.incl >> 32) };
-    asm volatile("ds_write_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" :: "v"(kept + (uint32_t)lane * 16), "v"(a) : "memory");
+    asm volatile("ds_write_b64 %0, %1\n\tds_write2_b32 %0, %2, %3 offset0:2 offset1:3\n\tds_write_b32 %0, %4 offset:16\n\ts_waitcnt lgkmcnt(0)"
+                 :: "v"(kept + (uint32_t)lane * 32), "v"(c.incl), "v"(c.L), "v"(c.M), "v"(c.q0) : "memory");
 }
 __device__ __forceinline__ Chunk kept_chunk(uint32_t kept, int lane)
 {
-    u32x4 a;
-    asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(a) : "v"(kept + (uint32_t)lane * 16) : "memory");
     Chunk c;
-    c.L = (int)a[0]; c.M = (int)a[1]; c.incl = (i64)((unsigned long long)a[3] << 32 | a[2]); c.bad = false;
+    asm volatile("ds_read_b64 %0, %4\n\tds_read_b32 %1, %4 offset:8\n\tds_read_b32 %2, %4 offset:12\n\tds_read_b32 %3, %4 offset:16\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(c.incl), "=&v"(c.L), "=&v"(c.M), "=&v"(c.q0) : "v"(kept + (uint32_t)lane * 32) : "memory");
+    c.bad = false;
     return c;
 }
 
@@ -119,7 +126,26 @@ struct Walk {
     i64 pos, end;                 // its share, and what comes next
     i64 head, wh;                 // where the current KV head's work begins; one head's work
     int h, team;                  // that head; the workgroup's place in the order of the shares
+    int part;                     // parts: tiles of a part (0: shares)
 };
+
+// The place in the order of `active` shares on each XCD, neighbours on one XCD; the others have no work, but say so.
+__device__ __forceinline__ int team_of(int per_xcd)
+{
+    const int xcd = blockIdx.x & 7, nth = blockIdx.x >> 3;
+    return nth < per_xcd ? xcd * per_xcd + nth : 8 * per_xcd + (nth - per_xcd) * 8 + xcd;
+}
+
+// n / d for 0 <= n, 1 <= d < 2^22 (the quotient by the reciprocal is off by one at most)
+__device__ __forceinline__ int divided(int n, int d, float inv)
+{
+    int q = (int)((float)n * inv);
+    const int r = n - q * d;
+    q += r >= d;
+    q -= r < 0;
+    return q;
+}
+__device__ __forceinline__ int parts_of(int t, int part, float inv) { return divided(t + part - 1, part, inv); }
 
 __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool leader, Chunk &c)
 {
@@ -132,28 +158,74 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
         all += lane_value(c.incl, 63);
     }
     if (leader && bad) atomicOr(p.flag, 2u);
+    k.head = 0; k.h = 0; k.part = 0;
     k.wh = all;
     all *= p.Hkv;
+    if (p.parts) {
+        // Few rows per request (all requests in this chunk, a block each): every part of at most `part` tiles has a workgroup of its own, with the smallest such number
+        // for which there are enough.  Where the longest request is so much longer than the average that two pieces per workgroup
+        // do better, shares it is.
+        const int t = c.M ? (c.L + c.M + 31) >> 5 : 0;
+        const int longest = [&] {
+            int x = t;
+#pragma unroll
+            for (int d = 32; d >= 1; d >>= 1) x = max(x, __shfl_xor(x, d));
+            return __builtin_amdgcn_readfirstlane(x);
+        }();
+        const int total = __builtin_amdgcn_readlane(wave_sums(t), 63) * p.Hkv;
+        const int average = (total + p.teams - 1) >> (31 - __builtin_clz(p.teams));
+        int lo = max(LEAST_PART, average), hi = max(longest, lo);
+        auto count = [&](int part) {
+            return __builtin_amdgcn_readlane(wave_sums(t ? parts_of(t, part, __builtin_amdgcn_rcpf((float)part)) : 0), 63) * p.Hkv;
+        };
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (count(mid) <= p.teams) hi = mid; else lo = mid + 1;
+        }
+        if (lo * 32 * PART <= average * 32 * PART + p.start) {
+            k.part = lo;
+            const int n = count(lo);
+            k.team = team_of((n + 7) >> 3);
+            k.pos = k.team; k.end = n;
+            return k;
+        }
+    }
     const int teams_log2 = 31 - __builtin_clz(p.teams);
     const i64 w = most((all + p.teams - 1) >> teams_log2, p.wmin);
     // as many shares on each XCD: where the work is for a part of the workgroups, all XCDs have some
-    const int xcd = blockIdx.x & 7, nth = blockIdx.x >> 3;
     int per_xcd = p.teams >> 3;
     if (w == p.wmin) per_xcd = min(per_xcd, (((int)all + p.wmin - 1) / p.wmin + 7) >> 3);       // (all is teams * wmin at most)
-    if (nth < per_xcd) {
-        k.team = xcd * per_xcd + nth;
-        k.pos = least(k.team * w, all);
-        k.end = least(k.pos + w, all);
-    } else {
-        k.team = 8 * per_xcd + (nth - per_xcd) * 8 + xcd;               // (the others have no work, but say so)
-        k.pos = k.end = all;
-    }
-    k.head = 0; k.h = 0;
+    k.team = team_of(per_xcd);
+    k.pos = least(k.team * w, all);
+    k.end = least(k.pos + w, all);
     return k;
 }
 
+// The only piece of a workgroup in the form of parts: part i of n of a request's tiles, cut behind even numbers of them (a round of two waves).
+__device__ __forceinline__ bool only_piece(const ChunkParams &p, Walk &k, const Chunk &c, Piece &pc, Req &rq, Left &left)
+{
+    if (k.pos >= k.end) return false;
+    const int t = c.M ? (c.L + c.M + 31) >> 5 : 0;
+    const float inv = __builtin_amdgcn_rcpf((float)k.part);
+    const int mine = t ? parts_of(t, k.part, inv) : 0, upto = wave_sums(mine), all = __builtin_amdgcn_readlane(upto, 63);
+    const int x = (int)k.pos, h = divided(x, all, __builtin_amdgcn_rcpf((float)all)), y = x - h * all;
+    const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(y < upto));
+    const int n = __builtin_amdgcn_readlane(mine, src), i = y - (__builtin_amdgcn_readlane(upto, src) - n), tiles = __builtin_amdgcn_readlane(t, src);
+    const float by = __builtin_amdgcn_rcpf((float)n);
+    auto cut = [&](int at) { return at == 0 ? 0 : at == n ? tiles : divided(tiles * at, n, by) & ~1; };
+    rq.q0 = __builtin_amdgcn_readlane(c.q0, src); rq.L = __builtin_amdgcn_readlane(c.L, src); rq.M = __builtin_amdgcn_readlane(c.M, src);
+    pc.rq = src; pc.g = __builtin_amdgcn_readfirstlane(h); pc.by = 0; pc.bx = 0; pc.node0 = 0; pc.nodes = rq.M;
+    pc.st0 = __builtin_amdgcn_readfirstlane(cut(i)); pc.st1 = __builtin_amdgcn_readfirstlane(cut(i + 1));
+    pc.direct = n == 1;
+    pc.prow0 = (2 * k.team + (i == 0 ? 1 : 0)) * p.wr;
+    if (n > 1 && i == 0) { left.flags = BEGUN; left.row0 = rq.q0; left.nodes = rq.M; left.g = pc.g; }
+    if (n > 1 && i == n - 1) left.flags = ENDED;
+    k.pos = k.end;
+    return true;
+}
+
 // The next piece; the walk moves behind it.  False: none left.  c holds the first chunk of requests.
-__device__ __forceinline__ bool next_piece(const ChunkParams &p, Walk &k, int lane, const Chunk &c, Piece &pc, Left &left)
+__device__ __forceinline__ bool next_piece(const ChunkParams &p, Walk &k, int lane, const Chunk &c, Piece &pc, Req &rq, Left &left)
 {
     while (k.pos < k.end) {
         while (k.pos - k.head >= k.wh) { k.head += k.wh; ++k.h; }
@@ -167,37 +239,44 @@ __device__ __forceinline__ bool next_piece(const ChunkParams &p, Walk &k, int la
             d = load_chunk(p, r0, lane, lane_value(d.incl, 63));
         }
         const int src = __builtin_ctzll(beyond);
-        const int L = __builtin_amdgcn_readlane(d.L, src), M = __builtin_amdgcn_readlane(d.M, src);
+        const int L = __builtin_amdgcn_readlane(d.L, src), M = __builtin_amdgcn_readlane(d.M, src), q0 = __builtin_amdgcn_readlane(d.q0, src);
         const i64 y = x - (lane_value(d.incl, src) - length_of(p, L, M));              // place in the request's work
-        const int whole = M / p.nb;
+        const int whole = quotient(M, p.nb, p.inv_nb);
         // the block: the largest b with length_to(b) <= y, from the quadratic's root
-        const double q1 = START + (double)WHOLE * L + 0.5 * WHOLE * p.nb, q2 = 0.5 * WHOLE * p.nb;
-        int b = __builtin_amdgcn_readfirstlane((int)fmin((sqrt(q1 * q1 + 4.0 * q2 * (double)y) - q1) / (2.0 * q2), (double)whole));
-        while (b > 0 && length_to(p, L, b) > y) --b;
-        while (b < whole && length_to(p, L, b + 1) <= y) ++b;
+        int b = 0;
+        if (whole > 0) {
+            const float q1 = (float)p.start + (float)WHOLE * (float)L + 0.5f * WHOLE * (float)p.nb, yf = (float)y;
+            const float root = 2.0f * yf / (q1 + __builtin_amdgcn_sqrtf(q1 * q1 + 2.0f * WHOLE * (float)p.nb * yf));
+            b = min(__builtin_amdgcn_readfirstlane((int)root), whole);
+            while (b > 0 && length_to(p, L, b) > y) --b;
+            while (b < whole && length_to(p, L, b + 1) <= y) ++b;
+        }
         const int node0 = b * p.nb, nodes = min(p.nb, M - node0), keys = L + node0 + nodes, t = (keys + 31) >> 5;
         const int wt = b < whole ? WHOLE : part_weight(p, nodes);
         const int y0 = (int)(y - length_to(p, L, b)), cl = wt * keys, cm = MARGIN * 32 * wt;
         const i64 us = k.pos - y0;
+        rq.q0 = q0; rq.L = L; rq.M = M;
         pc.rq = r0 + src; pc.g = k.h; pc.by = b; pc.node0 = node0; pc.nodes = nodes;
         pc.bx = 0; pc.st0 = 0; pc.st1 = t; pc.direct = 1;
         if (t <= SMALL) {                               // to the share in which it begins
-            k.pos = us + START + cl;
+            k.pos = us + p.start + cl;
             if (y0 == 0) return true;
             continue;
         }
-        const i64 ts = us + START;
-        int c0 = y0 - START, c1 = (int)least(k.end - ts, cl);
+        const i64 ts = us + p.start;
+        int c0 = y0 - p.start, c1 = (int)least(k.end - ts, cl);
         c0 = c0 < cm ? 0 : c0 > cl - cm ? cl : c0;
         c1 = c1 < cm ? 0 : c1 > cl - cm ? cl : c1;
         k.pos = c1 < cl ? k.end : ts + cl;
         if (c0 >= c1) continue;
-        pc.st0 = c0 / 32 / wt;
-        pc.st1 = c1 == cl ? t : c1 / 32 / wt;
+        auto tile = [&](int x) { return wt == WHOLE ? (int)(__umulhi((uint32_t)x, 0xAAAAAAABu) >> 6) : x >> 6; };      // x / (32 wt)
+        static_assert(WHOLE == 3 && PART == 2, "the quotients above");
+        pc.st0 = tile(c0);
+        pc.st1 = c1 == cl ? t : tile(c1);
         const bool first = c0 == 0, last = c1 == cl;
         pc.direct = first && last;
         pc.prow0 = (2 * k.team + (first ? 1 : 0)) * p.wr;
-        if (first && !last) { left.flags |= BEGUN; left.rq = pc.rq; left.g = pc.g; left.by = b; }
+        if (first && !last) { left.flags |= BEGUN; left.row0 = q0 + node0; left.nodes = nodes; left.g = k.h; }
         if (!first && last) left.flags |= ENDED;
         return true;
     }
@@ -211,7 +290,7 @@ __global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams
     // (every argument in one round trip)
     asm volatile("" ::"s"(p.Q), "s"(p.K), "s"(p.V), "s"(p.O), "s"(p.block_table), "s"(p.q_offset), "s"(p.prefix_len), "s"(p.Opart), "s"(p.ML), "s"(p.flag), "s"(p.M),
                  "s"(p.L), "s"(p.Hq), "s"(p.Hkv), "s"(p.G), "s"(p.ginv), "s"(p.max_blocks), "s"(p.num_blocks), "s"(p.total_M), "s"(p.batch), "s"(p.wmin),
-                 "s"(p.scale_log2), "s"(p.out_scale), "s"(p.left), "s"(p.nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys));
+                 "s"(p.scale_log2), "s"(p.out_scale), "s"(p.left), "s"(p.nb), "s"(p.inv_nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys), "s"(p.start), "s"(p.parts));
     Chunk c;
     Walk k = share_out(p, threadIdx.x & 63, blockIdx.x == 0 && threadIdx.x < 64, c);
     using CL = ChunkLds<D, RW, KW, NT, EB>;
@@ -226,9 +305,8 @@ __global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams
             c = CL::KEPT ? kept_chunk(kept, tid & 63) : load_chunk(p, 0, tid & 63, 0);
         }
         Piece pc = {};
-        if (!next_piece(p, k, tid & 63, c, pc, left)) break;
-        const Span s = load_span(p, pc.rq);
-        const Req rq = { s.q0, s.M, s.L, true };
+        Req rq = {};
+        if (!(k.part ? only_piece(p, k, c, pc, rq, left) : next_piece(p, k, tid & 63, c, pc, rq, left))) break;
         attn_piece<D, RW, KW, NT, true, EB, true>(p, smem, tid, rq, pc, [] {});
         // every wave is done with this piece's LDS, its own fills have landed; the stores may still be on their way
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -237,62 +315,84 @@ __global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams
     if (threadIdx.x == 0) p.left[k.team] = left;
 }
 
-// The blocks that were cut: 16 lanes per row, 16 rows per workgroup; workgroup (k, slice) looks at the block that share k has begun.  Parts are added in the order of
+// The blocks that were cut: 16 lanes per row, ROWS rows per workgroup; workgroup (k, slice) looks at the block that share k has begun.  Parts are added in the order of
 // their keys, each relative to the row's largest reference; they come in fp16 beside their magnitude (attn_piece.h), sums are fp32.
+constexpr int MERGE_ROWS = 32;
 template <int D>
 __global__ __launch_bounds__(256) void chunk_merge(ChunkParams p)
 {
-    constexpr int E = D / 16;
+    constexpr int E = D / 16, R = MERGE_ROWS / 16;
     typedef _Float16 hvec __attribute__((ext_vector_type(E)));
     typedef __bf16 bvec __attribute__((ext_vector_type(E)));
-    const int k = blockIdx.x, lane = threadIdx.x & 63;
+    asm volatile("" ::"s"(p.left), "s"(p.teams), "s"(p.wr), "s"(p.G), "s"(p.ginv), "s"(p.ML), "s"(p.Opart), "s"(p.O), "s"(p.Hq), "s"(p.out_scale));
+    const int k = blockIdx.x, lane = threadIdx.x & 63, sub = threadIdx.x & 15;
     const Left left = p.left[k];
-    if (!(left.flags & BEGUN)) return;
+    const int next = p.left[min(k + 1 + lane, p.teams - 1)].flags;
+    if (!(left.flags & BEGUN) || (int)blockIdx.y * MERGE_ROWS >= left.nodes * p.G) return;
     // the first share behind k that ends a block ends this one (those between lie within it)
-    int n = 0;
-    for (int k0 = k + 1;; k0 += 64) {
-        const int at = k0 + lane;
-        const unsigned long long ended = __builtin_amdgcn_ballot_w64(at >= p.teams || (p.left[min(at, p.teams - 1)].flags & ENDED));
+    int n = 2;
+    unsigned long long ended = __builtin_amdgcn_ballot_w64(k + 1 + lane < p.teams && (next & ENDED));
+    for (int k0 = k + 1;;) {
         if (ended) { n = k0 - k + __builtin_ctzll(ended) + 1; break; }
+        k0 += 64;
+        if (k0 >= p.teams) return;                      // (cannot be)
+        ended = __builtin_amdgcn_ballot_w64(k0 + lane < p.teams && (p.left[min(k0 + lane, p.teams - 1)].flags & ENDED));
     }
-    if (k + n > p.teams) return;                        // (cannot be)
-    const Span s = load_span(p, left.rq);
-    const int node0 = left.by * p.nb, nodes = min(p.nb, s.M - node0), x = blockIdx.y * 16 + (threadIdx.x >> 4), node = (x * p.ginv) >> 16;
-    if (node >= nodes) return;
-    const int sub = threadIdx.x & 15;
-    auto row_of = [&](int i) { return (size_t)(2 * (k + i) + (i == 0)) * p.wr + x; };
-    float mmax = NEG_BIG;
-    for (int i = sub; i < n; i += 16) mmax = fmaxf(mmax, p.ML[row_of(i) * 4]);
+    const int x0 = blockIdx.y * MERGE_ROWS + (threadIdx.x >> 4);
+    auto row_of = [&](int i, int r) { return (size_t)(2 * (k + i) + (i == 0)) * p.wr + x0 + 16 * r; };
+    float mmax[R], den[R], acc[R][E];
 #pragma unroll
-    for (int d = 8; d >= 1; d >>= 1) mmax = fmaxf(mmax, __shfl_xor(mmax, d));
-    float acc[E], den = 0.f;
+    for (int r = 0; r < R; ++r) {
+        mmax[r] = NEG_BIG; den[r] = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+        for (int e = 0; e < E; ++e) acc[r][e] = 0.f;
+    }
+    // up to four parts are asked for at once; the reference follows from batch to batch
     for (int i0 = 0; i0 < n; i0 += 4) {
-        hvec part[4];
-        float4 ml[4];
+        hvec part[R][4];
+        float4 ml[R][4];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const size_t row = row_of(min(i0 + b, n - 1));
-            ml[b] = *reinterpret_cast<const float4 *>(p.ML + row * 4);
-            part[b] = *reinterpret_cast<const hvec *>(p.Opart + row * D + sub * E);
-        }
+        for (int b = 0; b < 4; ++b)
+            if (i0 + b < n)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const float w = i0 + b < n ? __builtin_amdgcn_exp2f(ml[b].x - mmax) : 0.f;
-            den += w * ml[b].y;
-            const float wa = w * ml[b].z;
-            if (wa != 0.f)                              // (a part that the row sees none of has nothing to add)
+                for (int r = 0; r < R; ++r) {
+                    const size_t row = row_of(i0 + b, r);
+                    ml[r][b] = *reinterpret_cast<const float4 *>(p.ML + row * 4);
+                    part[r][b] = *reinterpret_cast<const hvec *>(p.Opart + row * D + sub * E);
+                }
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] = fmaf(wa, (float)part[b][e], acc[e]);
+        for (int r = 0; r < R; ++r) {
+            float mn = mmax[r];
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                if (i0 + b < n) mn = fmaxf(mn, ml[r][b].x);
+            const float alpha = __builtin_amdgcn_exp2f(mmax[r] - mn);
+            mmax[r] = mn;
+            den[r] *= alpha;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[r][e] *= alpha;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                if (i0 + b < n) {
+                    const float w = __builtin_amdgcn_exp2f(ml[r][b].x - mn), wa = w * ml[r][b].z;
+                    den[r] += w * ml[r][b].y;
+                    if (wa != 0.f)                      // (a part that the row sees none of has nothing to add)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) acc[r][e] = fmaf(wa, (float)part[r][b][e], acc[r][e]);
+                }
         }
     }
-    const float inv = p.out_scale / den;
-    bvec o;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = (__bf16)(acc[e] * inv);
-    const size_t orow = (size_t)(s.q0 + node0 + node) * p.Hq + left.g * p.G + (x - node * p.G);
-    *reinterpret_cast<bvec *>(static_cast<__bf16 *>(p.O) + orow * D + sub * E) = o;
+    for (int r = 0; r < R; ++r) {
+        const int x = x0 + 16 * r, node = (x * p.ginv) >> 16;
+        if (node >= left.nodes) continue;
+        const float inv = p.out_scale / den[r];
+        bvec o;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = (__bf16)(acc[r][e] * inv);
+        const size_t orow = (size_t)(left.row0 + node) * p.Hq + left.g * p.G + (x - node * p.G);
+        *reinterpret_cast<bvec *>(static_cast<__bf16 *>(p.O) + orow * D + sub * E) = o;
+    }
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
@@ -304,9 +404,9 @@ int check_chunk(int batch, int M_max, int L_max, int Hq, int Hkv, int D)
     BTV_REQUIRE(L_max >= 0 && (i64)L_max + M_max < (1ll << 29), "L_max=%d out of range", L_max);         // (weighted lengths of a block stay in 32 bits)
     BTV_REQUIRE(Hq >= 1 && Hkv >= 1 && Hkv <= 1024 && Hq % Hkv == 0 && Hq / Hkv <= 16, "bad heads Hq=%d Hkv=%d", Hq, Hkv);
     BTV_REQUIRE(D == 64 || D == 128, "D=%d not in {64,128}", D);
-    // the work's length stays in 62 bits: per request and head at most M/4 + 1 blocks
-    const double block = START + (double)WHOLE * ((double)L_max + M_max);
-    BTV_REQUIRE((double)batch * Hkv * (M_max / 4 + 1) * block < 4.0e18, "more work than can be counted");
+    // the work's length stays below 2^62, and 64 requests' of one head below 2^54 (a request and head has at most M / 4 + 1 blocks)
+    const double head = (M_max / 4 + 1) * (4096.0 + (double)WHOLE * ((double)L_max + M_max));
+    BTV_REQUIRE(64 * head < 1.8e16 && batch * head * Hkv < 4.6e18, "more work than can be counted");
     return BTV_OK;
 }
 
@@ -318,6 +418,9 @@ int rows_per_block(int M_max, int G, int eb)
 }
 int teams_of(int wr) { return wr == 64 ? 512 : 256; }           // one workgroup per CU, or two of the small ones
 bool cuts(int M_max, int L_max) { return (L_max + M_max + 31) / 32 > SMALL; }
+
+// What a row block costs besides its keys, in tiles of whole blocks: finding it, its first loads, its last steps and stores.
+int start_of(int wr, int D, int eb) { return wr == 64 ? 14 : eb == 1 ? 13 : D == 64 ? 9 : 7; }
 
 struct WsLayout { size_t left, ml, opart, total; };
 WsLayout ws_layout(int wr, int D, bool cut)
@@ -388,8 +491,10 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     p.max_blocks = max_blocks; p.num_blocks = num_blocks; p.total_M = total_M; p.batch = batch;
     p.scale_log2 = factor; p.out_scale = v_scale;
     p.left = reinterpret_cast<Left *>(w8 + wl.left);
-    p.wr = wr; p.nb = wr / G; p.teams = teams_of(wr);
-    p.wmin = 2 * START;
+    p.wr = wr; p.nb = wr / G; p.inv_nb = reciprocal(p.nb); p.teams = teams_of(wr);
+    p.start = start_of(wr, D, eb) * 32 * WHOLE;
+    p.wmin = p.start + 8 * 32 * WHOLE;
+    p.parts = M_max <= p.nb && batch <= 64 && batch * Hkv <= p.teams;
     p.most_keys = (int)std::min<i64>((i64)max_blocks * BTV_PAGE, INT_MAX);
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define BTV_CASE(DD, EE, RR, KK, NN) if (D == DD && eb == EE && wr == RR * 32) rc = launch<DD, RR, KK, NN, EE>(p, st); else
@@ -399,7 +504,7 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     return btv_fail(BTV_EINVAL, "no kernel for D=%d", D);
 #undef BTV_CASE
     if (rc || !cut) return rc;
-    const dim3 grid(p.teams, wr / 16);
+    const dim3 grid(p.teams, wr / MERGE_ROWS);
     if (D == 64) hipLaunchKernelGGL(chunk_merge<64>, grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL(chunk_merge<128>, grid, dim3(256), 0, st, p);
     BTV_HIP(hipGetLastError());
