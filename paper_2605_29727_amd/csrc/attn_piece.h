@@ -240,7 +240,8 @@ __device__ __forceinline__ int fill_key_off(int w, int jj, int l)
 // JB .. JE - 1: which of the wave's LPW fills (all by default; the pipelined loop issues them one by one, each behind a
 // group of MFMAs, because an issue holds its wave for about a hundred cycles).
 // PGV: the page comes from lane `at` of the window in f.pages, else from a scalar load.
-template <int D, int WAVES, bool PAGED, int EB = 2, int JB = 0, int JE = Lds<D, EB>::INSTR / WAVES, bool PGV = false>
+// GIVEN: `at` is the page's id.
+template <int D, int WAVES, bool PAGED, int EB = 2, int JB = 0, int JE = Lds<D, EB>::INSTR / WAVES, bool PGV = false, bool GIVEN = false>
 __device__ __forceinline__ void issue_tile(const Fill<D, WAVES, PAGED, EB> &f, unsigned char *smem, int slot, int st, int w, int l, int at = 0)
 {
     using LD = Lds<D, EB>;
@@ -248,6 +249,7 @@ __device__ __forceinline__ void issue_tile(const Fill<D, WAVES, PAGED, EB> &f, u
     const bool whole = kb + 32 <= f.S;       // uniform: no key of this tile needs clamping
     const unsigned char *src;                // uniform
     if constexpr (!PAGED) src = f.base + (size_t)kb * f.row_bytes;
+    else if constexpr (GIVEN) src = f.page(f.valid_page(at));
     else if constexpr (PGV) src = f.page(__builtin_amdgcn_readlane((int)f.pages, at));
     else {
         src = f.page(f.valid_page(f.page_id(st)));
@@ -998,6 +1000,17 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
     // rounds; an issue holds its wave for about a hundred cycles, so a full prefill would only delay the start.
     constexpr int PREFILL = WL::PREFILL;
     int issued = st0, islot = 0;
+    if constexpr (CAUSAL) {                              // (the first pages' ids in one round trip: one after the other they are 1.5 us of a piece)
+        int id[PREFILL];
+#pragma unroll
+        for (int k = 0; k < PREFILL; ++k) id[k] = fill.page_id(st0 + k);
+#pragma unroll
+        for (int k = 0; k < PREFILL; ++k)
+            if (issued < st1) {
+                issue_tile<D, WAVES, PAGED, EB, 0, LPW, false, true>(fill, smem, islot, issued, wu, l, id[k]);
+                ++issued; ++islot;
+            }
+    } else
 #pragma unroll
     for (int k = 0; k < PREFILL; ++k)
         if (issued < st1) {

@@ -8,129 +8,130 @@
 // either), and its share of the requests' new table entries.  Latency bounds it: the launch, the lengths' round trip, the pages' round trip.
 #include "btv_common.h"
 
+#include <atomic>
 #include <climits>
 
 namespace {
 
-constexpr int THREADS = 256, WAVES = THREADS / 64, MOST_REQUESTS = 4096, PER_THREAD = MOST_REQUESTS / THREADS;
+constexpr int THREADS = 256, WAVES = THREADS / 64, MOST_REQUESTS = 4096;
 
 struct ExtendParams {
     const int32_t *prefix_len, *n_new, *depth, *n_pages, *free_pages, *n_free;
     int32_t *block_table, *q_offset, *slot, *position, *n_pages_out, *n_free_out;
     uint32_t *flag;
-    int batch, total_max, num_blocks, max_blocks, rows_per_wg, per_thread;
+    int batch, total_max, num_blocks, max_blocks, rows_per_wg;
 };
 
-struct Need { int L, M, P, take; bool ok; };
+// What is kept of a request in LDS for the rows: where its rows begin, its length and pages, and how many pages were taken before it (-1 where it does not get
+// what it needs).
+struct Kept { int32_t *first, *L, *P, *taken; };
 
-__device__ __forceinline__ Need need_of(const ExtendParams &p, int r)
+// Inclusive sums over the lanes (numbers below 2^54 in three pieces).
+__device__ __forceinline__ int wave_sums(int x)
 {
-    Need n;
-    n.L = p.prefix_len[r]; n.M = p.n_new[r]; n.P = p.n_pages[r];
-    const long long have = (long long)p.max_blocks * BTV_PAGE;
-    n.ok = n.L >= 0 && n.M >= 0 && (long long)n.L + n.M <= have && n.P >= 0 && n.P <= p.max_blocks && (n.L + (BTV_PAGE - 1)) / BTV_PAGE <= n.P;
-    n.M = max(n.M, 0);
-    n.take = n.ok ? max((int)(((long long)n.L + n.M + (BTV_PAGE - 1)) / BTV_PAGE) - n.P, 0) : 0;
-    return n;
-}
-
-__device__ __forceinline__ long long wave_inclusive(long long x, int lane)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const long long y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+#define BTV_SCAN_STEP(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xF, ctrl < 0x142)
+    BTV_SCAN_STEP(0x111, 0xF); BTV_SCAN_STEP(0x112, 0xF); BTV_SCAN_STEP(0x114, 0xF); BTV_SCAN_STEP(0x118, 0xF);
+    BTV_SCAN_STEP(0x142, 0xA); BTV_SCAN_STEP(0x143, 0xC);
+#undef BTV_SCAN_STEP
     return x;
+}
+__device__ __forceinline__ long long wave_sums(long long x)
+{
+    constexpr int B = 18;
+    const long long lo = wave_sums((int)x & ((1 << B) - 1)), mid = wave_sums((int)(x >> B) & ((1 << B) - 1)), hi = wave_sums((int)(x >> 2 * B));
+    return lo + (mid << B) + (hi << 2 * B);
 }
 
 __global__ __launch_bounds__(THREADS) void paged_extend_kernel(ExtendParams p)
 {
     extern __shared__ int32_t lds[];
-    int32_t *first = lds;                              // [batch + 1]: where a request's rows begin
-    int32_t *taken = lds + p.batch + 1;                // [batch]: pages taken before it, or -1 where it gets none of what it needs
-    __shared__ long long sums[2][WAVES];
+    const Kept kept = { lds, lds + p.batch + 1, lds + 2 * p.batch + 1, lds + 3 * p.batch + 1 };
+    __shared__ long long sums[2][WAVES], given[WAVES];
+    asm volatile("" ::"s"(p.prefix_len), "s"(p.n_new), "s"(p.depth), "s"(p.n_pages), "s"(p.free_pages), "s"(p.n_free), "s"(p.block_table), "s"(p.q_offset), "s"(p.slot),
+                 "s"(p.position), "s"(p.n_pages_out), "s"(p.n_free_out), "s"(p.flag), "s"(p.batch), "s"(p.total_max), "s"(p.num_blocks), "s"(p.max_blocks));
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int n_free = *p.n_free;
     const bool bad_list = n_free < 0 || n_free > p.num_blocks;
     if (bad_list) n_free = 0;
-
-    // a thread has per_thread neighbouring requests
-    const int r0 = tid * p.per_thread, r1 = min(r0 + p.per_thread, p.batch);
-    long long rows = 0, pages = 0;
-    for (int r = r0; r < r1; ++r) {
-        const Need n = need_of(p, r);
-        rows += n.M; pages += n.take;
-    }
-    const long long rows_incl = wave_inclusive(rows, lane), pages_incl = wave_inclusive(pages, lane);
-    if (lane == 63) { sums[0][wave] = rows_incl; sums[1][wave] = pages_incl; }
-    __syncthreads();
-    long long at = rows_incl - rows, page = pages_incl - pages;
-    for (int w = 0; w < wave; ++w) { at += sums[0][w]; page += sums[1][w]; }
     bool bad = bad_list;
-    long long given = 0;
-    for (int r = r0; r < r1; ++r) {
-        const Need n = need_of(p, r);
-        const bool granted = n.ok && (n.take == 0 || page + n.take <= n_free);
-        first[r] = (int32_t)min(at, (long long)INT_MAX);
-        taken[r] = granted ? (int32_t)min(page, (long long)n_free) : -1;
-        if (granted) given += n.take;
-        bad = bad || !granted || at + n.M > p.total_max;
-        if (blockIdx.x == 0) {
-            p.q_offset[r] = first[r];
-            p.n_pages_out[r] = granted ? n.P + n.take : n.P;
+
+    // The requests, a turn of one per thread after the other; at, pages: sums up to the turn.
+    long long at = 0, pages = 0, taken_all = 0;
+    for (int r0 = 0; r0 < p.batch; r0 += THREADS) {
+        const int r = r0 + tid, rc = min(r, p.batch - 1);
+        const bool in = r < p.batch;
+        int L = p.prefix_len[rc], M = p.n_new[rc], P = p.n_pages[rc];
+        const long long have = (long long)p.max_blocks * BTV_PAGE;
+        const bool ok = L >= 0 && M >= 0 && (long long)L + M <= have && P >= 0 && P <= p.max_blocks && (L + (BTV_PAGE - 1)) / BTV_PAGE <= P;
+        M = in ? max(M, 0) : 0;
+        const int take = in && ok ? max((int)(((long long)L + M + (BTV_PAGE - 1)) / BTV_PAGE) - P, 0) : 0;
+        const long long m = wave_sums((long long)M), t = wave_sums((long long)take);
+        if (lane == 63) { sums[0][wave] = m; sums[1][wave] = t; }
+        __syncthreads();
+        long long row = at + m - M, page = pages + t - take;
+        for (int w = 0; w < WAVES; ++w) {
+            at += sums[0][w]; pages += sums[1][w];
+            if (w < wave) { row += sums[0][w]; page += sums[1][w]; }
         }
-        at += n.M; page += n.take;
-        if (r == p.batch - 1) {
-            first[p.batch] = (int32_t)min(at, (long long)INT_MAX);
-            if (blockIdx.x == 0) p.q_offset[p.batch] = first[p.batch];
+        if (in) {
+            const bool granted = ok && (take == 0 || page + take <= n_free);
+            const int first = row < INT_MAX ? (int)row : INT_MAX;
+            kept.first[r] = first; kept.L[r] = L; kept.P[r] = P;
+            kept.taken[r] = granted ? (page < n_free ? (int)page : n_free) : -1;
+            if (granted) taken_all += take;
+            bad = bad || !granted || row + M > p.total_max;
+            if (blockIdx.x == 0) {
+                p.q_offset[r] = first;
+                p.n_pages_out[r] = granted ? P + take : P;
+            }
         }
+        __syncthreads();                               // (the sums have been read; behind the last turn: what is kept is there)
     }
-    given = wave_inclusive(given, lane);
-    __syncthreads();                                   // (the sums have been read, first and taken are there)
+    const int total = at < INT_MAX ? (int)at : INT_MAX;
     if (blockIdx.x == 0) {
-        if (lane == 63) sums[0][wave] = given;
+        taken_all = wave_sums(taken_all);
+        if (lane == 63) given[wave] = taken_all;
         __syncthreads();
         if (tid == 0) {
             long long g = 0;
-            for (int w = 0; w < WAVES; ++w) g += sums[0][w];
+            for (int w = 0; w < WAVES; ++w) g += given[w];
             *p.n_free_out = (int32_t)(n_free - g);
+            p.q_offset[p.batch] = total;
         }
     }
 
-    // the table's new entries: a wavefront per request
-    for (int r = blockIdx.x * WAVES + wave; r < p.batch; r += gridDim.x * WAVES) {
-        const int base = taken[r];
-        if (base < 0) continue;
-        const Need n = need_of(p, r);
-        for (int k = lane; k < n.take; k += 64) {
-            const int id = p.free_pages[n_free - 1 - base - k];
-            bad = bad || id < 0 || id >= p.num_blocks;
-            p.block_table[(size_t)r * p.max_blocks + n.P + k] = id;
-        }
-    }
-
-    const int total = first[p.batch];
-    const long long b0 = (long long)blockIdx.x * p.rows_per_wg, b1 = min(b0 + p.rows_per_wg, (long long)p.total_max);
-    for (long long row = b0 + tid; row < b1; row += THREADS) {
+    auto row = [&](long long row) {
         int slot = -1, position = 0;
         if (row < total) {
             int lo = 0, hi = p.batch;                  // first[lo] <= row < first[hi]
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (first[mid] <= row) lo = mid; else hi = mid;
+                if (kept.first[mid] <= row) lo = mid; else hi = mid;
             }
-            const int i = (int)row - first[lo], L = p.prefix_len[lo], P = p.n_pages[lo], base = taken[lo];
-            const long long j = (long long)L + i;      // its place in the request
+            const int L = kept.L[lo], P = kept.P[lo], base = kept.taken[lo];
             if (base >= 0) {
-                position = p.depth ? L + p.depth[row] - 1 : (int)j;
-                const int b = (int)(j / BTV_PAGE);
+                const int j = L + ((int)row - kept.first[lo]), b = j / BTV_PAGE;       // its place in the request
                 const int id = b < P ? p.block_table[(size_t)lo * p.max_blocks + b] : p.free_pages[n_free - 1 - base - (b - P)];
-                if (id >= 0 && id < p.num_blocks) slot = id * BTV_PAGE + (int)(j % BTV_PAGE); else bad = true;
+                position = p.depth ? L + p.depth[row] - 1 : j;
+                if (id >= 0 && id < p.num_blocks) slot = id * BTV_PAGE + j % BTV_PAGE; else bad = true;
             }
         }
         p.slot[row] = slot;
         p.position[row] = position;
+    };
+    const long long b0 = (long long)blockIdx.x * p.rows_per_wg, b1 = min(b0 + p.rows_per_wg, (long long)p.total_max);
+    for (long long x = b0 + tid; x < b1; x += THREADS) row(x);
+
+    // The table's new entries: a wavefront per request (M again from where the next one's rows begin).
+    for (int r = blockIdx.x * WAVES + wave; r < p.batch; r += gridDim.x * WAVES) {
+        const int base = kept.taken[r], L = kept.L[r], P = kept.P[r];
+        if (base < 0) continue;
+        const int M = (r + 1 < p.batch ? kept.first[r + 1] : total) - kept.first[r], take = (L + M + (BTV_PAGE - 1)) / BTV_PAGE - P;
+        for (int k = lane; k < take; k += 64) {
+            const int id = p.free_pages[n_free - 1 - base - k];
+            bad = bad || id < 0 || id >= p.num_blocks;
+            p.block_table[(size_t)r * p.max_blocks + P + k] = id;
+        }
     }
     if (bad && p.flag) atomicOr(p.flag, 16u);
 }
@@ -154,11 +155,21 @@ extern "C" int btv_paged_extend(const int32_t *prefix_len, const int32_t *n_new,
     p.block_table = block_table; p.q_offset = q_offset; p.slot = slot; p.position = position; p.n_pages_out = n_pages_out; p.n_free_out = n_free_out;
     p.flag = static_cast<uint32_t *>(ws);
     p.batch = batch; p.total_max = total_max; p.num_blocks = num_blocks; p.max_blocks = max_blocks;
-    p.per_thread = (batch + THREADS - 1) / THREADS;
     // a thread per row while that is two workgroups per CU at most
     const int wgs = total_max <= THREADS ? 1 : total_max <= 512 * THREADS ? (total_max + THREADS - 1) / THREADS : 512;
     p.rows_per_wg = (int)(((long long)total_max + wgs - 1) / wgs);
-    hipLaunchKernelGGL(paged_extend_kernel, dim3(wgs), dim3(THREADS), (2 * batch + 1) * sizeof(int32_t), static_cast<hipStream_t>(stream), p);
+    const size_t bytes = (4 * (size_t)batch + 1) * sizeof(int32_t);
+    if (bytes > 60 * 1024) {                                    // (more than a workgroup gets unasked)
+        static std::atomic<unsigned long long> configured{0};   // a bit per device
+        int dev = 0;
+        BTV_HIP(hipGetDevice(&dev));
+        const unsigned long long bit = 1ull << (dev & 63);
+        if (!(configured.load(std::memory_order_acquire) & bit)) {
+            BTV_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(paged_extend_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (4 * MOST_REQUESTS + 1) * sizeof(int32_t)));
+            configured.fetch_or(bit, std::memory_order_release);
+        }
+    }
+    hipLaunchKernelGGL(paged_extend_kernel, dim3(wgs), dim3(THREADS), bytes, static_cast<hipStream_t>(stream), p);
     BTV_HIP(hipGetLastError());
     return BTV_OK;
 }

@@ -6,6 +6,7 @@
 // (of which fp32 keeps 2^-25) goes to the sine and cosine.  The rotation is in fp32; a result is rounded once, to the type it is stored in.
 #include "btv_common.h"
 
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -20,59 +21,140 @@ struct RopeParams {
     uint32_t *flag;
     long long num_slots;
     int total, Hq, Hkv, R, interleaved;
+    int units, inv_units, rotated, heads_per_pass, slices;      // see rope_append_kernel
     float factor, inv_k, inv_v;                        // E4M3 caches: 1 / scale
 };
 
-// The simplest form: a thread per (row, head, pair of channels) and per (row, head, channel) that is not rotated.
-template <typename T> __device__ __forceinline__ float load1(const void *p, long long i) { return (float)static_cast<const T *>(p)[i]; }
-template <typename T> __device__ __forceinline__ void store1(void *p, long long i, float x)
+// Eight neighbouring channels, 16 bytes of bf16 (32 of fp32), as they are loaded and as numbers.
+template <typename T> struct Eight { uint4 w[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ Eight<T> load8(const T *p)
 {
-    if constexpr (std::is_same_v<T, uint8_t>) {
-        x = x > 448.f ? 448.f : x < -448.f ? -448.f : x;
-        static_cast<uint8_t *>(p)[i] = (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xFF);
+    Eight<T> e;
+#pragma unroll
+    for (unsigned k = 0; k < sizeof(T) / 2; ++k) e.w[k] = reinterpret_cast<const uint4 *>(p)[k];
+    return e;
+}
+template <typename T> __device__ __forceinline__ void numbers(const Eight<T> &e, float (&x)[8])
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            x[4 * k] = __uint_as_float(e.w[k].x); x[4 * k + 1] = __uint_as_float(e.w[k].y);
+            x[4 * k + 2] = __uint_as_float(e.w[k].z); x[4 * k + 3] = __uint_as_float(e.w[k].w);
+        }
     } else {
-        static_cast<T *>(p)[i] = (T)x;
+        const uint32_t w[4] = { e.w[0].x, e.w[0].y, e.w[0].z, e.w[0].w };
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+    }
+}
+// (E4M3: times 1 / scale, limited to the largest code; no number stays none)
+template <typename C> __device__ __forceinline__ void store8(C *p, const float (&x)[8], float inv)
+{
+    if constexpr (std::is_same_v<C, uint8_t>) {
+        uint32_t w[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { const float v = x[4 * k + i] * inv; y[i] = v > 448.f ? 448.f : v < -448.f ? -448.f : v; }
+            w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
+        }
+        *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+    } else if constexpr (sizeof(C) == 4) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) reinterpret_cast<float4 *>(p)[k] = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+    } else {
+        typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+        bf16x8 y;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] = (__bf16)x[k];
+        *reinterpret_cast<bf16x8 *>(p) = y;
     }
 }
 
-template <typename T, typename C, int D>
+// A wavefront has one row, or one of `slices` shares of its heads.  A lane has the same channels of head after head, so that its angles are worked out once: eight
+// channels, and with halves the eight that they pair up with; channels that are not rotated go in eights of their own.  A pass of the wavefront takes as many heads as
+// its lanes have room for (eight of 128 channels, all rotated), the next pass's loads are under way meanwhile.  Bound by HBM: 8191 rows of 32 + 2 x 8 heads of 128 channels, bf16, 201 MB
+// in 45 us.
+template <typename T, typename C, int D, bool PAIRS_SIDE_BY_SIDE>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeParams p)
 {
-    const int row = blockIdx.x, heads = p.Hq + 2 * p.Hkv;
+    constexpr bool SIDE = PAIRS_SIDE_BY_SIDE;
+    constexpr int ANGLES = SIDE ? 4 : 8;
+    const int wave = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int row = wave / p.slices, slice = wave - row * p.slices;
+    if (row >= p.total) return;
     const int slot = p.slot[row];
     const bool stored = slot >= 0 && slot < p.num_slots;
-    if (slot >= p.num_slots && threadIdx.x == 0 && p.flag) atomicOr(p.flag, 32u);
-    const double pos = (double)p.position[row];
-    for (int e = threadIdx.x; e < heads * (D / 2); e += 256) {
-        const int head = e / (D / 2), i = e % (D / 2);
-        const bool isq = head < p.Hq, isv = head >= p.Hq + p.Hkv;
-        const int h = isq ? head : isv ? head - p.Hq - p.Hkv : head - p.Hq;
-        if (!isq && !stored) continue;
-        const void *src = isq ? p.Q : isv ? p.V : p.K;
-        const long long from = (isq ? p.q_stride : isv ? p.v_stride : p.k_stride) * row + (long long)h * D;
-        const bool rotated = !isv && i < p.R / 2;
-        int a, b;                                      // (channels past the first R and values: two neighbours of what is left)
-        if (rotated) { a = p.interleaved ? 2 * i : i; b = p.interleaved ? 2 * i + 1 : i + p.R / 2; }
-        else { a = 2 * i; b = 2 * i + 1; }
-        float x = load1<T>(src, from + a), y = load1<T>(src, from + b);
-        if (rotated) {
-            double turns = pos * (p.inv_freq[i] * 0.15915494309189533577);
-            turns -= rint(turns);
-            float s, c;
-            sincospif(2.0f * (float)turns, &s, &c);
-            s *= p.factor; c *= p.factor;
-            const float u = x * c - y * s;
-            y = x * s + y * c;
-            x = u;
+    if (slot >= p.num_slots && slice == 0 && lane == 0 && p.flag) atomicOr(p.flag, 32u);
+    const int units = p.units, rotated = p.rotated;                   // of a head: eights (with halves pairs of eights), of which the first are rotated
+    const int h0 = (lane * p.inv_units) >> 16, u = lane - h0 * units; // (lane < 64: exact)
+    const bool turns_ = u < rotated, live = h0 < p.heads_per_pass;
+    const int c0 = turns_ || SIDE ? 8 * u : p.R + 8 * (u - rotated), c1 = c0 + p.R / 2;
+    const T *Q = static_cast<const T *>(p.Q) + p.q_stride * row, *K = static_cast<const T *>(p.K) + p.k_stride * row, *V = static_cast<const T *>(p.V) + p.v_stride * row;
+    C *Kc = static_cast<C *>(p.Kc) + (long long)slot * p.Hkv * D, *Vc = static_cast<C *>(p.Vc) + (long long)slot * p.Hkv * D;
+    T *Qo = static_cast<T *>(p.Qout) + (long long)row * p.Hq * D;
+    const int step = p.heads_per_pass * p.slices, heads = p.Hq + (stored ? p.Hkv : 0);
+
+    Eight<T> a = {}, b = {};
+    auto load = [&](int h) {
+        if (!live || h >= heads) return;
+        const T *src = h < p.Hq ? Q + h * D : K + (h - p.Hq) * D;
+        a = load8(src + c0);
+        if (!SIDE && turns_) b = load8(src + c1);
+    };
+    int h = slice * p.heads_per_pass + h0;
+    load(h);
+    // the values, as they are: their loads and stores are under way while the angles are worked out
+    if (stored)
+        for (int e = slice * 64 + lane; e < p.Hkv * (D / 8); e += 64 * p.slices) {
+            float x[8];
+            numbers(load8(V + e * 8), x);
+            store8(Vc + e * 8, x, p.inv_v);
+        }
+    float sn[ANGLES], cs[ANGLES];
+    if (live && turns_) {
+        const double pos = (double)p.position[row];
+#pragma unroll
+        for (int k = 0; k < ANGLES; ++k) {
+            double t = pos * (p.inv_freq[ANGLES * u + k] * 0.15915494309189533577);
+            t -= rint(t);
+            sincospif(2.0f * (float)t, &sn[k], &cs[k]);
+            sn[k] *= p.factor; cs[k] *= p.factor;
+        }
+    }
+    for (; h - h0 < heads; h += step) {
+        const Eight<T> a0 = a, b0 = b;
+        load(h + step);
+        if (!live || h >= heads) continue;
+        const bool isq = h < p.Hq;
+        float x[8], y[8];
+        numbers(a0, x);
+        if (turns_) {
+            if constexpr (SIDE) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float v = x[2 * k], w = x[2 * k + 1];
+                    x[2 * k] = v * cs[k] - w * sn[k];
+                    x[2 * k + 1] = v * sn[k] + w * cs[k];
+                }
+            } else {
+                numbers(b0, y);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float v = x[k], w = y[k];
+                    x[k] = v * cs[k] - w * sn[k];
+                    y[k] = v * sn[k] + w * cs[k];
+                }
+            }
         }
         if (isq) {
-            const long long to = ((long long)row * p.Hq + h) * D;
-            store1<T>(p.Qout, to + a, x); store1<T>(p.Qout, to + b, y);
+            store8(Qo + h * D + c0, x, 1.0f);
+            if (!SIDE && turns_) store8(Qo + h * D + c1, y, 1.0f);
         } else {
-            const long long to = ((long long)slot * p.Hkv + h) * D;
-            const float f = std::is_same_v<C, uint8_t> ? isv ? p.inv_v : p.inv_k : 1.0f;
-            void *cache = isv ? p.Vc : p.Kc;
-            store1<C>(cache, to + a, x * f); store1<C>(cache, to + b, y * f);
+            store8(Kc + (h - p.Hq) * D + c0, x, p.inv_k);
+            if (!SIDE && turns_) store8(Kc + (h - p.Hq) * D + c1, y, p.inv_k);
         }
     }
 }
@@ -96,18 +178,25 @@ int rope_append(RopeParams p, int dtype, int eb, int D, void *stream)
     BTV_REQUIRE(p.q_stride % per16 == 0 && p.k_stride % per16 == 0 && p.v_stride % per16 == 0, "rows must be multiples of 16 bytes apart");
     BTV_REQUIRE(p.total == 1 || (p.q_stride >= (long long)p.Hq * D && p.k_stride >= (long long)p.Hkv * D && p.v_stride >= (long long)p.Hkv * D), "rows overlap");
     BTV_REQUIRE(p.Qout != p.Q || p.total == 1 || p.q_stride == (long long)p.Hq * D, "Qout may be Q only where its rows follow each other");
-    const dim3 grid(p.total);
+    p.rotated = p.interleaved ? p.R / 8 : p.R / 16;
+    p.units = p.rotated + (D - p.R) / 8;
+    p.inv_units = (65536 + p.units - 1) / p.units;
+    p.heads_per_pass = 64 / p.units;
+    // Few rows: a row's passes over several wavefronts, up to two on each of the 1024 SIMDs
+    const int passes = (p.Hq + p.Hkv + p.heads_per_pass - 1) / p.heads_per_pass;
+    p.slices = std::max(1, std::min(passes, 2048 / p.total));
+    const dim3 grid((unsigned)(((long long)p.total * p.slices + 3) / 4));
     hipStream_t st = static_cast<hipStream_t>(stream);
-#define BTV_CASE(DT, EB, DD, T, C)                                                                       \
-    if (dtype == DT && eb == EB && D == DD) {                                                            \
-        hipLaunchKernelGGL((rope_append_kernel<T, C, DD>), grid, dim3(256), 0, st, p);                   \
-        BTV_HIP(hipGetLastError());                                                                      \
-        return BTV_OK;                                                                                   \
+#define BTV_CASE(DT, EB, DD, T, C)                                                                                       \
+    if (dtype == DT && eb == EB && D == DD) {                                                                            \
+        if (p.interleaved) hipLaunchKernelGGL((rope_append_kernel<T, C, DD, true>), grid, dim3(256), 0, st, p);          \
+        else hipLaunchKernelGGL((rope_append_kernel<T, C, DD, false>), grid, dim3(256), 0, st, p);                       \
+        BTV_HIP(hipGetLastError());                                                                                      \
+        return BTV_OK;                                                                                                   \
     }
     BTV_CASE(BTV_F32, 4, 64, float, float) BTV_CASE(BTV_F32, 4, 128, float, float)
     BTV_CASE(BTV_BF16, 2, 64, __bf16, __bf16) BTV_CASE(BTV_BF16, 2, 128, __bf16, __bf16)
-    BTV_CASE(BTV_BF16, 1, 128, __bf16, uint8_t)
-    BTV_CASE(BTV_BF16, 1, 64, __bf16, uint8_t)
+    BTV_CASE(BTV_BF16, 1, 64, __bf16, uint8_t) BTV_CASE(BTV_BF16, 1, 128, __bf16, uint8_t)
 #undef BTV_CASE
     return btv_fail(BTV_EINVAL, "an E4M3 cache takes bfloat16 rows");
 }
