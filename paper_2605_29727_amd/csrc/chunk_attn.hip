@@ -23,7 +23,7 @@ typedef long long i64;
 
 constexpr int WHOLE = 3, PART = 2;                              // weights of a key
 constexpr int MARGIN = 2, SMALL = 8;                            // tiles: a cut nearer to a block's ends moves there; blocks of up to SMALL are not cut
-constexpr int LEAST_PART = 4;                                   // tiles of the smallest part of a token's keys
+constexpr int LEAST_PART = 4;                                   // tiles of the smallest part
 constexpr int MOST_ROWS = 1 << 20, MOST_TEAMS = 512;
 
 // What a workgroup leaves for the merge: whether it has begun a block that others carry on with (and where that one's rows are), and whether the block
@@ -39,7 +39,7 @@ struct ChunkParams : AttnParams {
     int teams;                    // workgroups: 256 or 512
     int start;                    // what a row block costs besides its keys
     int most_keys;                // what a row of the block table has room for
-    int parts;                    // whether every request is one row block, and all of them and their parts may have workgroups of their own
+    int weight;                   // of a key, for the largest request's blocks
 };
 
 // 64-bit minimum and maximum of numbers less than 2^62 apart, by the sign of their difference.  (Of values that a wavefront has in common the compiler makes a vector
@@ -161,37 +161,36 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
     k.head = 0; k.h = 0; k.part = 0;
     k.wh = all;
     all *= p.Hkv;
-    if (p.parts) {
-        // Few rows per request (all requests in this chunk, a block each): every part of at most `part` tiles has a workgroup of its own, with the smallest such number
-        // for which there are enough.  Where the longest request is so much longer than the average that two pieces per workgroup
-        // do better, shares it is.
-        const int t = c.M ? (c.L + c.M + 31) >> 5 : 0;
-        const int longest = [&] {
-            int x = t;
-#pragma unroll
-            for (int d = 32; d >= 1; d >>= 1) x = max(x, __shfl_xor(x, d));
-            return __builtin_amdgcn_readfirstlane(x);
-        }();
-        const int total = __builtin_amdgcn_readlane(wave_sums(t), 63) * p.Hkv;
-        const int average = (total + p.teams - 1) >> (31 - __builtin_clz(p.teams));
-        int lo = max(LEAST_PART, average), hi = max(longest, lo);
-        auto count = [&](int part) {
-            return __builtin_amdgcn_readlane(wave_sums(t ? parts_of(t, part, __builtin_amdgcn_rcpf((float)part)) : 0), 63) * p.Hkv;
-        };
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (count(mid) <= p.teams) hi = mid; else lo = mid + 1;
-        }
-        if (lo * 32 * PART <= average * 32 * PART + p.start) {
-            k.part = lo;
-            const int n = count(lo);
-            k.team = team_of((n + 7) >> 3);
-            k.pos = k.team; k.end = n;
-            return k;
-        }
-    }
     const int teams_log2 = 31 - __builtin_clz(p.teams);
     const i64 w = most((all + p.teams - 1) >> teams_log2, p.wmin);
+    if (p.batch <= 64) {
+        // Few blocks: every part of at most `part` tiles has a workgroup of its own, with the smallest such number for which there are enough (all blocks of a request go in as
+        // many parts as its last).  A share costs its length and START for what it carries on with, a part its tiles and START: where requests differ so
+        // much that the longest part takes longer, shares it is.
+        const int blocks = quotient(c.M + p.nb - 1, p.nb, p.inv_nb), t = c.M ? (c.L + c.M + 31) >> 5 : 0;
+        const i64 all_blocks = lane_value(wave_sums_of_lengths(blocks), 63) * p.Hkv;
+        if (all_blocks <= p.teams && all_blocks > 0) {
+            int longest = t;
+#pragma unroll
+            for (int d = 32; d >= 1; d >>= 1) longest = max(longest, __shfl_xor(longest, d));
+            longest = __builtin_amdgcn_readfirstlane(longest);
+            int lo = (int)most((lane_value(wave_sums_of_lengths((i64)blocks * t), 63) * p.Hkv) >> teams_log2, LEAST_PART), hi = max(longest, lo);
+            auto count = [&](int part) {
+                return __builtin_amdgcn_readlane(wave_sums(t ? blocks * parts_of(t, part, __builtin_amdgcn_rcpf((float)part)) : 0), 63) * p.Hkv;
+            };
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (count(mid) <= p.teams) hi = mid; else lo = mid + 1;
+            }
+            if ((i64)lo * 32 * p.weight <= w && longest < 1 << 20) {     // (beyond, a cut's place would leave 32 bits)
+                k.part = lo;
+                const int n = count(lo);
+                k.team = team_of((n + 7) >> 3);
+                k.pos = k.team; k.end = n;
+                return k;
+            }
+        }
+    }
     // as many shares on each XCD: where the work is for a part of the workgroups, all XCDs have some
     int per_xcd = p.teams >> 3;
     if (w == p.wmin) per_xcd = min(per_xcd, (((int)all + p.wmin - 1) / p.wmin + 7) >> 3);       // (all is teams * wmin at most)
@@ -201,28 +200,32 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
     return k;
 }
 
-// The only piece of a workgroup in the form of parts: part i of n of a request's tiles, cut behind even numbers of them (a round of two waves).
+// The only piece of a workgroup in the form of parts: part i of n of a block's tiles, cut behind even numbers of them (a round of two waves).
 __device__ __forceinline__ bool only_piece(const ChunkParams &p, Walk &k, const Chunk &c, Piece &pc, Req &rq, Left &left)
 {
     if (k.pos >= k.end) return false;
-    const int t = c.M ? (c.L + c.M + 31) >> 5 : 0;
-    const float inv = __builtin_amdgcn_rcpf((float)k.part);
-    const int mine = t ? parts_of(t, k.part, inv) : 0, upto = wave_sums(mine), all = __builtin_amdgcn_readlane(upto, 63);
-    const int x = (int)k.pos, h = divided(x, all, __builtin_amdgcn_rcpf((float)all)), y = x - h * all;
+    const int parts = c.M ? parts_of((c.L + c.M + 31) >> 5, k.part, __builtin_amdgcn_rcpf((float)k.part)) : 0;
+    const int mine = quotient(c.M + p.nb - 1, p.nb, p.inv_nb) * parts, upto = wave_sums(mine), all = __builtin_amdgcn_readlane(upto, 63);
+    const int x = (int)k.pos, h = __builtin_amdgcn_readfirstlane(divided(x, all, __builtin_amdgcn_rcpf((float)all))), y = x - h * all;
     const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(y < upto));
-    const int n = __builtin_amdgcn_readlane(mine, src), i = y - (__builtin_amdgcn_readlane(upto, src) - n), tiles = __builtin_amdgcn_readlane(t, src);
-    const float by = __builtin_amdgcn_rcpf((float)n);
-    auto cut = [&](int at) { return at == 0 ? 0 : at == n ? tiles : divided(tiles * at, n, by) & ~1; };
+    const int at = y - (__builtin_amdgcn_readlane(upto, src) - __builtin_amdgcn_readlane(mine, src)), most_parts = __builtin_amdgcn_readlane(parts, src);
+    const int b = __builtin_amdgcn_readfirstlane(divided(at, most_parts, __builtin_amdgcn_rcpf((float)most_parts))), i = at - b * most_parts;
     rq.q0 = __builtin_amdgcn_readlane(c.q0, src); rq.L = __builtin_amdgcn_readlane(c.L, src); rq.M = __builtin_amdgcn_readlane(c.M, src);
-    pc.rq = src; pc.g = __builtin_amdgcn_readfirstlane(h); pc.by = 0; pc.bx = 0; pc.node0 = 0; pc.nodes = rq.M;
-    pc.st0 = __builtin_amdgcn_readfirstlane(cut(i)); pc.st1 = __builtin_amdgcn_readfirstlane(cut(i + 1));
+    const int node0 = b * p.nb, nodes = min(p.nb, rq.M - node0), t = (rq.L + node0 + nodes + 31) >> 5;
+    const int n = t <= SMALL ? 1 : min(most_parts, t / LEAST_PART);      // (a block of few keys: fewer parts, the other workgroups have nothing)
+    k.pos = k.end;
+    if (i >= n) return false;
+    const float inv = __builtin_amdgcn_rcpf((float)n);
+    auto cut = [&](int at) { return at == 0 ? 0 : at == n ? t : __builtin_amdgcn_readfirstlane(divided(t * at, n, inv)) & ~1; };
+    pc.rq = src; pc.g = h; pc.by = b; pc.bx = 0; pc.node0 = node0; pc.nodes = nodes;
+    pc.st0 = cut(i); pc.st1 = cut(i + 1);
     pc.direct = n == 1;
     pc.prow0 = (2 * k.team + (i == 0 ? 1 : 0)) * p.wr;
-    if (n > 1 && i == 0) { left.flags = BEGUN; left.row0 = rq.q0; left.nodes = rq.M; left.g = pc.g; }
+    if (n > 1 && i == 0) { left.flags = BEGUN; left.row0 = rq.q0 + node0; left.nodes = nodes; left.g = h; }
     if (n > 1 && i == n - 1) left.flags = ENDED;
-    k.pos = k.end;
     return true;
 }
+static_assert(LEAST_PART >= 4, "a part is of two tiles or more after its cuts are moved to even numbers");
 
 // The next piece; the walk moves behind it.  False: none left.  c holds the first chunk of requests.
 __device__ __forceinline__ bool next_piece(const ChunkParams &p, Walk &k, int lane, const Chunk &c, Piece &pc, Req &rq, Left &left)
@@ -290,7 +293,7 @@ __global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams
     // (every argument in one round trip)
     asm volatile("" ::"s"(p.Q), "s"(p.K), "s"(p.V), "s"(p.O), "s"(p.block_table), "s"(p.q_offset), "s"(p.prefix_len), "s"(p.Opart), "s"(p.ML), "s"(p.flag), "s"(p.M),
                  "s"(p.L), "s"(p.Hq), "s"(p.Hkv), "s"(p.G), "s"(p.ginv), "s"(p.max_blocks), "s"(p.num_blocks), "s"(p.total_M), "s"(p.batch), "s"(p.wmin),
-                 "s"(p.scale_log2), "s"(p.out_scale), "s"(p.left), "s"(p.nb), "s"(p.inv_nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys), "s"(p.start), "s"(p.parts));
+                 "s"(p.scale_log2), "s"(p.out_scale), "s"(p.left), "s"(p.nb), "s"(p.inv_nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys), "s"(p.start), "s"(p.weight));
     Chunk c;
     Walk k = share_out(p, threadIdx.x & 63, blockIdx.x == 0 && threadIdx.x < 64, c);
     using CL = ChunkLds<D, RW, KW, NT, EB>;
@@ -420,7 +423,7 @@ int teams_of(int wr) { return wr == 64 ? 512 : 256; }           // one workgroup
 bool cuts(int M_max, int L_max) { return (L_max + M_max + 31) / 32 > SMALL; }
 
 // What a row block costs besides its keys, in tiles of whole blocks: finding it, its first loads, its last steps and stores.
-int start_of(int wr, int D, int eb) { return wr == 64 ? 14 : eb == 1 ? 13 : D == 64 ? 9 : 7; }
+int start_of(int wr, int D, int eb) { return wr == 64 ? 14 : eb == 1 ? 16 : D == 64 ? 12 : 9; }
 
 struct WsLayout { size_t left, ml, opart, total; };
 WsLayout ws_layout(int wr, int D, bool cut)
@@ -494,7 +497,7 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     p.wr = wr; p.nb = wr / G; p.inv_nb = reciprocal(p.nb); p.teams = teams_of(wr);
     p.start = start_of(wr, D, eb) * 32 * WHOLE;
     p.wmin = p.start + 8 * 32 * WHOLE;
-    p.parts = M_max <= p.nb && batch <= 64 && batch * Hkv <= p.teams;
+    p.weight = (i64)M_max * G * 2 <= wr ? PART : WHOLE;
     p.most_keys = (int)std::min<i64>((i64)max_blocks * BTV_PAGE, INT_MAX);
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define BTV_CASE(DD, EE, RR, KK, NN) if (D == DD && eb == EE && wr == RR * 32) rc = launch<DD, RR, KK, NN, EE>(p, st); else

@@ -107,7 +107,8 @@ SHAPE_IDS = ["bf16_d128", "bf16_d64", "fp8"]
 
 @pytest.mark.parametrize("kv,Hq,Hkv,D", SHAPES, ids=SHAPE_IDS)
 @pytest.mark.parametrize("Ls,Ms", [([0], [1]), ([37], [1]), ([15], [1]), ([16], [1]), ([31], [1]), ([32], [2]), ([0], [16]), ([0], [33]), ([63], [65]), ([5], [200]), ([1000], [64]),
-                                   ([96], [97]), ([3000], [1]), ([20000], [1]), ([9000], [17]), ([2500], [300]), ([0], [1030]), ([129], [511])],
+                                   ([96], [97]), ([100], [1]), ([159], [1]), ([190], [4]), ([223], [1]), ([255], [1]), ([256], [1]), ([290], [3]), ([0], [256]), ([0], [257]), ([60], [229]),
+                                   ([3000], [1]), ([20000], [1]), ([9000], [17]), ([700], [100]), ([1500], [150]), ([2500], [300]), ([0], [1030]), ([129], [511])],
                          ids=lambda x: "-".join(map(str, x)))
 def test_one_request(kv, Hq, Hkv, D, Ls, Ms):
     b = make(sum(Ls) + sum(Ms), Ls, Ms, Hq, Hkv, D, kv)
