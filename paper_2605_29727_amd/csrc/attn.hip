@@ -93,15 +93,6 @@ __global__ __launch_bounds__(256) void anc_mask_kernel(const int32_t *parent, in
 // * Words carry the call's tag (one more than `epoch`, which every workgroup reads at its start and whoever has seen all of the group
 //   moves on), so they are never cleared and a workspace may change its sizes from call to call.
 // An exchange between 32 workgroups takes 930 cycles through the L2 and 2300 at the memory side (MI355X, store to all have read).
-constexpr int MERGE_GROUPS = 128, MERGE_SPLITS = 32;
-typedef unsigned long long u64;
-struct MergeWords {                                     // of one group
-    u64 started[MERGE_SPLITS];                          // tag << 8 | XCD
-    u64 near[MERGE_SPLITS], far[MERGE_SPLITS];          // tag << 8 | 1 if it has left
-    u64 epoch, pad[31];
-};
-static_assert(sizeof(MergeWords) == 1024, "whole cache lines per group");
-static_assert(MERGE_GROUPS * sizeof(MergeWords) == MERGE_WORDS, "calls of other forms leave them alone");
 constexpr int MERGE_WAIT_TICKS = 2000;                  // 20 us of the 100 MHz wall clock
 constexpr int MERGE_START_TICKS = 500;                  // (see "not started" above)
 

@@ -19,7 +19,17 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int TK = 32;          // keys per tile = per LDS stage
-constexpr size_t MERGE_WORDS = 128 * 1024;      // behind a workspace's header: words that one request's merge keeps from call to call, whatever other attention calls do with the rest
+// Behind a workspace's header: words that attention calls keep from call to call, whatever others do with the rest.
+constexpr int MERGE_GROUPS = 128, MERGE_SPLITS = 32;
+typedef unsigned long long u64;
+struct MergeWords {                                     // of one group: the merge inside one request's kernel
+    u64 started[MERGE_SPLITS];                          // tag << 8 | XCD
+    u64 near[MERGE_SPLITS], far[MERGE_SPLITS];          // tag << 8 | 1 if it has left
+    u64 epoch;
+    u64 arrived[31];                                    // chunks: parts of a block that are stored, 0 between calls
+};
+static_assert(sizeof(MergeWords) == 1024, "whole cache lines per group");
+constexpr size_t MERGE_WORDS = MERGE_GROUPS * sizeof(MergeWords);
 constexpr float NEG_BIG = -1.0e30f;
 
 struct AttnParams {
@@ -888,6 +898,7 @@ template <int B> __device__ __forceinline__ float finite_max(f32x16 (&x)[B])
 }
 
 // What one workgroup does in one go: rows of row block `by` of (request, KV head g) against the tiles st0 .. st1 - 1.
+constexpr int COHERENT = 16;            // of a buffer access: SC1, at the scope of the device
 struct Piece {
     int rq, g, by, st0, st1;
     int bx;                       // which partial of its rows this is
@@ -897,6 +908,7 @@ struct Piece {
     // chunks only
     int node0, nodes;             // the row block's nodes
     int prow0;                    // where its partial's rows begin
+    bool through;                 // whether they are stored past this XCD's caches
 };
 
 // A page window (32 tiles' page ids) per 256 bytes, four of them in turn, behind everything else; not where two workgroups
@@ -1615,6 +1627,24 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
             const h2 lo = { (_Float16)fin[dt][q * 4 + 0], (_Float16)fin[dt][q * 4 + 1] }, hi = { (_Float16)fin[dt][q * 4 + 2], (_Float16)fin[dt][q * 4 + 3] };
             return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
         };
+        if constexpr (CAUSAL && RW == 2)
+            if (pc_.through) {
+                // (few rows, within the first 2^31 bytes)
+                const auto rows = __builtin_amdgcn_make_buffer_rsrc(p.Opart, 0, 0x7FFFFFFF, 0x00027000), ml = __builtin_amdgcn_make_buffer_rsrc(p.ML, 0, 0x7FFFFFFF, 0x00027000);
+#pragma unroll
+                for (int dt = 0; dt < DTK; ++dt)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint2 a = pack(dt, q);
+                        const u32x2 w = { a.x, a.y };
+                        __builtin_amdgcn_raw_buffer_store_b64(w, rows, (int)((prow * D + (dt0 + dt) * 32 + 8 * q + 4 * h) * 2), 0, COHERENT);
+                    }
+                if (h == 0 && kw == 0) {
+                    const u32x4 w = { __float_as_uint(m_run), __float_as_uint(l_run), __float_as_uint(amax), 0u };
+                    __builtin_amdgcn_raw_buffer_store_b128(w, ml, (int)(prow * 16), 0, COHERENT);
+                }
+                return;
+            }
         store_rows(reinterpret_cast<unsigned char *>(p.Opart) + (prow * D + dt0 * 32) * 2, pack);
         if (h == 0 && kw == 0) *reinterpret_cast<float4 *>(p.ML + prow * 4) = make_float4(m_run, l_run, amax, 0.f);
     }

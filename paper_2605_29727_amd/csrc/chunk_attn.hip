@@ -24,7 +24,8 @@ typedef long long i64;
 constexpr int WHOLE = 3, PART = 2;                              // weights of a key
 constexpr int MARGIN = 2, SMALL = 8;                            // tiles: a cut nearer to a block's ends moves there; blocks of up to SMALL are not cut
 constexpr int LEAST_PART = 4;                                   // tiles of the smallest part
-constexpr int MOST_ROWS = 1 << 20, MOST_TEAMS = 512;
+constexpr int MOST_ROWS = 1 << 20, MOST_TEAMS = 1024;
+constexpr int FEW_ROWS = 16;                                   // of a block whose parts the workgroups merge themselves
 
 // What a workgroup leaves for the merge: whether it has begun a block that others carry on with (and where that one's rows are), and whether the block
 // that it carried on with ends with its part.
@@ -36,10 +37,11 @@ struct ChunkParams : AttnParams {
     int nb;                       // nodes per row block
     uint32_t inv_nb;              // for quotient()
     int wr;                       // rows per row block
-    int teams;                    // workgroups: 256 or 512
+    int teams;                    // workgroups: a power of two
     int start;                    // what a row block costs besides its keys
     int most_keys;                // what a row of the block table has room for
     int weight;                   // of a key, for the largest request's blocks
+    MergeWords *words;            // parts always, merged by the workgroup that stores the last of a block's (null: by a launch of its own)
 };
 
 // 64-bit minimum and maximum of numbers less than 2^62 apart, by the sign of their difference.  (Of values that a wavefront has in common the compiler makes a vector
@@ -74,6 +76,14 @@ __device__ __forceinline__ i64 wave_sums_of_lengths(i64 x)
     constexpr int B = 18;
     const i64 lo = wave_sums((int)x & ((1 << B) - 1)), mid = wave_sums((int)(x >> B) & ((1 << B) - 1)), hi = wave_sums((int)(x >> 2 * B));
     return lo + (mid << B) + (hi << 2 * B);
+}
+__device__ __forceinline__ int wave_max(int x)             // (not negative)
+{
+#define BTV_MAX_STEP(ctrl, rows) x = max(x, __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xF, ctrl < 0x142))
+    BTV_MAX_STEP(0x111, 0xF); BTV_MAX_STEP(0x112, 0xF); BTV_MAX_STEP(0x114, 0xF); BTV_MAX_STEP(0x118, 0xF);
+    BTV_MAX_STEP(0x142, 0xA); BTV_MAX_STEP(0x143, 0xC);
+#undef BTV_MAX_STEP
+    return __builtin_amdgcn_readlane(x, 63);
 }
 __device__ __forceinline__ i64 lane_value(i64 x, int lane)
 {
@@ -168,23 +178,26 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
         // many parts as its last).  A share costs its length and START for what it carries on with, a part its tiles and START: where requests differ so
         // much that the longest part takes longer, shares it is.
         const int blocks = quotient(c.M + p.nb - 1, p.nb, p.inv_nb), t = c.M ? (c.L + c.M + 31) >> 5 : 0;
-        const i64 all_blocks = lane_value(wave_sums_of_lengths(blocks), 63) * p.Hkv;
+        const int all_blocks = __builtin_amdgcn_readlane(wave_sums(blocks), 63) * p.Hkv;
         if (all_blocks <= p.teams && all_blocks > 0) {
-            int longest = t;
-#pragma unroll
-            for (int d = 32; d >= 1; d >>= 1) longest = max(longest, __shfl_xor(longest, d));
-            longest = __builtin_amdgcn_readfirstlane(longest);
-            int lo = (int)most((lane_value(wave_sums_of_lengths((i64)blocks * t), 63) * p.Hkv) >> teams_log2, LEAST_PART), hi = max(longest, lo);
-            auto count = [&](int part) {
-                return __builtin_amdgcn_readlane(wave_sums(t ? blocks * parts_of(t, part, __builtin_amdgcn_rcpf((float)part)) : 0), 63) * p.Hkv;
-            };
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (count(mid) <= p.teams) hi = mid; else lo = mid + 1;
+            const int longest = wave_max(t);
+            // (not below what the work comes to for each, rounded down)
+            int lo = max(LEAST_PART, (int)((float)(all - (i64)all_blocks * p.start) * (0.999f / 32) / (float)(p.weight * p.teams))), n = all_blocks;
+            // what parts save has to be worth their merge
+            if ((longest - lo) * 32 * p.weight < p.start / 4) lo = max(lo, longest);
+            else {
+                int hi = longest;
+                auto count = [&](int part) {
+                    return __builtin_amdgcn_readlane(wave_sums(t ? blocks * parts_of(t, part, __builtin_amdgcn_rcpf((float)part)) : 0), 63) * p.Hkv;
+                };
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (count(mid) <= p.teams) hi = mid; else lo = mid + 1;
+                }
+                n = count(lo);
             }
-            if ((i64)lo * 32 * p.weight <= w && longest < 1 << 20) {     // (beyond, a cut's place would leave 32 bits)
+            if (p.words || ((i64)lo * 32 * p.weight <= w && longest < 1 << 20)) {      // (beyond, a cut's place would leave 32 bits)
                 k.part = lo;
-                const int n = count(lo);
                 k.team = team_of((n + 7) >> 3);
                 k.pos = k.team; k.end = n;
                 return k;
@@ -201,7 +214,8 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
 }
 
 // The only piece of a workgroup in the form of parts: part i of n of a block's tiles, cut behind even numbers of them (a round of two waves).
-__device__ __forceinline__ bool only_piece(const ChunkParams &p, Walk &k, const Chunk &c, Piece &pc, Req &rq, Left &left)
+// n, i: what is cut, and which part this is.
+__device__ __forceinline__ bool only_piece(const ChunkParams &p, Walk &k, const Chunk &c, Piece &pc, Req &rq, Left &left, int &n, int &i)
 {
     if (k.pos >= k.end) return false;
     const int parts = c.M ? parts_of((c.L + c.M + 31) >> 5, k.part, __builtin_amdgcn_rcpf((float)k.part)) : 0;
@@ -209,10 +223,11 @@ __device__ __forceinline__ bool only_piece(const ChunkParams &p, Walk &k, const 
     const int x = (int)k.pos, h = __builtin_amdgcn_readfirstlane(divided(x, all, __builtin_amdgcn_rcpf((float)all))), y = x - h * all;
     const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(y < upto));
     const int at = y - (__builtin_amdgcn_readlane(upto, src) - __builtin_amdgcn_readlane(mine, src)), most_parts = __builtin_amdgcn_readlane(parts, src);
-    const int b = __builtin_amdgcn_readfirstlane(divided(at, most_parts, __builtin_amdgcn_rcpf((float)most_parts))), i = at - b * most_parts;
+    const int b = __builtin_amdgcn_readfirstlane(divided(at, most_parts, __builtin_amdgcn_rcpf((float)most_parts)));
+    i = at - b * most_parts;
     rq.q0 = __builtin_amdgcn_readlane(c.q0, src); rq.L = __builtin_amdgcn_readlane(c.L, src); rq.M = __builtin_amdgcn_readlane(c.M, src);
     const int node0 = b * p.nb, nodes = min(p.nb, rq.M - node0), t = (rq.L + node0 + nodes + 31) >> 5;
-    const int n = t <= SMALL ? 1 : min(most_parts, t / LEAST_PART);      // (a block of few keys: fewer parts, the other workgroups have nothing)
+    n = t <= SMALL ? 1 : min(most_parts, t / LEAST_PART);      // (a block of few keys: fewer parts, the other workgroups have nothing)
     k.pos = k.end;
     if (i >= n) return false;
     const float inv = __builtin_amdgcn_rcpf((float)n);
@@ -220,7 +235,8 @@ __device__ __forceinline__ bool only_piece(const ChunkParams &p, Walk &k, const 
     pc.rq = src; pc.g = h; pc.by = b; pc.bx = 0; pc.node0 = node0; pc.nodes = nodes;
     pc.st0 = cut(i); pc.st1 = cut(i + 1);
     pc.direct = n == 1;
-    pc.prow0 = (2 * k.team + (i == 0 ? 1 : 0)) * p.wr;
+    pc.through = p.words != nullptr;
+    pc.prow0 = p.words ? k.team * FEW_ROWS : (2 * k.team + (i == 0 ? 1 : 0)) * p.wr;
     if (n > 1 && i == 0) { left.flags = BEGUN; left.row0 = rq.q0 + node0; left.nodes = nodes; left.g = h; }
     if (n > 1 && i == n - 1) left.flags = ENDED;
     return true;
@@ -286,63 +302,17 @@ __device__ __forceinline__ bool next_piece(const ChunkParams &p, Walk &k, int la
     return false;
 }
 
-template <int D, int RW, int KW, int NT, int EB>
-__global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams p)
+// Parts' rows, joined in the order of their keys, each relative to the row's largest reference.  16 lanes per row, R rows 16 apart per lane; row(i, r): where part i's
+// lie.  Parts come in fp16 beside their magnitude (attn_piece.h), sums are fp32.  Up to four parts are asked for at once; the reference follows from four to four.
+// THROUGH: past this XCD's caches, to which workgroups elsewhere did not write.
+template <int D, int R, bool THROUGH, typename Row, typename Store>
+__device__ __forceinline__ void join_parts(const ChunkParams &p, int n, int sub, Row row, Store store)
 {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    // (every argument in one round trip)
-    asm volatile("" ::"s"(p.Q), "s"(p.K), "s"(p.V), "s"(p.O), "s"(p.block_table), "s"(p.q_offset), "s"(p.prefix_len), "s"(p.Opart), "s"(p.ML), "s"(p.flag), "s"(p.M),
-                 "s"(p.L), "s"(p.Hq), "s"(p.Hkv), "s"(p.G), "s"(p.ginv), "s"(p.max_blocks), "s"(p.num_blocks), "s"(p.total_M), "s"(p.batch), "s"(p.wmin),
-                 "s"(p.scale_log2), "s"(p.out_scale), "s"(p.left), "s"(p.nb), "s"(p.inv_nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys), "s"(p.start), "s"(p.weight));
-    Chunk c;
-    Walk k = share_out(p, threadIdx.x & 63, blockIdx.x == 0 && threadIdx.x < 64, c);
-    using CL = ChunkLds<D, RW, KW, NT, EB>;
-    const uint32_t kept = (uint32_t)(uintptr_t)BTV_LDS_PTR(smem) + CL::PL::BYTES;
-    if (CL::KEPT && threadIdx.x < 64) keep_chunk(kept, threadIdx.x, c);     // (barriers before it is read: those of the first piece)
-    Left left = { 0, 0, 0, 0 };
-    for (bool again = false;; again = true) {
-        int tid = threadIdx.x;
-        asm volatile("" : "+v"(tid));                   // keeps what derives from it (all addresses) from being carried across pieces
-        if (again) {
-            if (k.pos >= k.end) break;
-            c = CL::KEPT ? kept_chunk(kept, tid & 63) : load_chunk(p, 0, tid & 63, 0);
-        }
-        Piece pc = {};
-        Req rq = {};
-        if (!(k.part ? only_piece(p, k, c, pc, rq, left) : next_piece(p, k, tid & 63, c, pc, rq, left))) break;
-        attn_piece<D, RW, KW, NT, true, EB, true>(p, smem, tid, rq, pc, [] {});
-        // every wave is done with this piece's LDS, its own fills have landed; the stores may still be on their way
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-    }
-    if (threadIdx.x == 0) p.left[k.team] = left;
-}
-
-// The blocks that were cut: 16 lanes per row, ROWS rows per workgroup; workgroup (k, slice) looks at the block that share k has begun.  Parts are added in the order of
-// their keys, each relative to the row's largest reference; they come in fp16 beside their magnitude (attn_piece.h), sums are fp32.
-constexpr int MERGE_ROWS = 32;
-template <int D>
-__global__ __launch_bounds__(256) void chunk_merge(ChunkParams p)
-{
-    constexpr int E = D / 16, R = MERGE_ROWS / 16;
+    constexpr int E = D / 16;
+    const auto ml_rsrc = __builtin_amdgcn_make_buffer_rsrc(p.ML, 0, MOST_TEAMS * FEW_ROWS * 16, 0x00027000);
+    const auto part_rsrc = __builtin_amdgcn_make_buffer_rsrc(p.Opart, 0, MOST_TEAMS * FEW_ROWS * D * 2, 0x00027000);
     typedef _Float16 hvec __attribute__((ext_vector_type(E)));
     typedef __bf16 bvec __attribute__((ext_vector_type(E)));
-    asm volatile("" ::"s"(p.left), "s"(p.teams), "s"(p.wr), "s"(p.G), "s"(p.ginv), "s"(p.ML), "s"(p.Opart), "s"(p.O), "s"(p.Hq), "s"(p.out_scale));
-    const int k = blockIdx.x, lane = threadIdx.x & 63, sub = threadIdx.x & 15;
-    const Left left = p.left[k];
-    const int next = p.left[min(k + 1 + lane, p.teams - 1)].flags;
-    if (!(left.flags & BEGUN) || (int)blockIdx.y * MERGE_ROWS >= left.nodes * p.G) return;
-    // the first share behind k that ends a block ends this one (those between lie within it)
-    int n = 2;
-    unsigned long long ended = __builtin_amdgcn_ballot_w64(k + 1 + lane < p.teams && (next & ENDED));
-    for (int k0 = k + 1;;) {
-        if (ended) { n = k0 - k + __builtin_ctzll(ended) + 1; break; }
-        k0 += 64;
-        if (k0 >= p.teams) return;                      // (cannot be)
-        ended = __builtin_amdgcn_ballot_w64(k0 + lane < p.teams && (p.left[min(k0 + lane, p.teams - 1)].flags & ENDED));
-    }
-    const int x0 = blockIdx.y * MERGE_ROWS + (threadIdx.x >> 4);
-    auto row_of = [&](int i, int r) { return (size_t)(2 * (k + i) + (i == 0)) * p.wr + x0 + 16 * r; };
     float mmax[R], den[R], acc[R][E];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -350,7 +320,6 @@ __global__ __launch_bounds__(256) void chunk_merge(ChunkParams p)
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[r][e] = 0.f;
     }
-    // up to four parts are asked for at once; the reference follows from batch to batch
     for (int i0 = 0; i0 < n; i0 += 4) {
         hvec part[R][4];
         float4 ml[R][4];
@@ -359,9 +328,15 @@ __global__ __launch_bounds__(256) void chunk_merge(ChunkParams p)
             if (i0 + b < n)
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    const size_t row = row_of(i0 + b, r);
-                    ml[r][b] = *reinterpret_cast<const float4 *>(p.ML + row * 4);
-                    part[r][b] = *reinterpret_cast<const hvec *>(p.Opart + row * D + sub * E);
+                    const size_t at = row(i0 + b, r);
+                    if constexpr (THROUGH) {
+                        ml[r][b] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(ml_rsrc, (int)at * 16, 0, COHERENT));
+                        if constexpr (E == 8) part[r][b] = __builtin_bit_cast(hvec, __builtin_amdgcn_raw_buffer_load_b128(part_rsrc, (int)at * D * 2 + sub * 16, 0, COHERENT));
+                        else part[r][b] = __builtin_bit_cast(hvec, __builtin_amdgcn_raw_buffer_load_b64(part_rsrc, (int)at * D * 2 + sub * 8, 0, COHERENT));
+                    } else {
+                        ml[r][b] = *reinterpret_cast<const float4 *>(p.ML + at * 4);
+                        part[r][b] = *reinterpret_cast<const hvec *>(p.Opart + at * D + sub * E);
+                    }
                 }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -387,15 +362,103 @@ __global__ __launch_bounds__(256) void chunk_merge(ChunkParams p)
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int x = x0 + 16 * r, node = (x * p.ginv) >> 16;
-        if (node >= left.nodes) continue;
         const float inv = p.out_scale / den[r];
         bvec o;
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] = (__bf16)(acc[r][e] * inv);
-        const size_t orow = (size_t)(left.row0 + node) * p.Hq + left.g * p.G + (x - node * p.G);
-        *reinterpret_cast<bvec *>(static_cast<__bf16 *>(p.O) + orow * D + sub * E) = o;
+        store(r, o);
     }
+}
+
+// Few rows: the workgroup that stores the last of a block's parts merges them all (each counts itself in; the count is back at 0 then).  Nothing waits: who is not last
+// leaves.  Rows and the count go to the memory side and come from there, where all XCDs see the same (a store is acknowledged when it is there, and only then its
+// workgroup counts itself in); with fences of the device in their place every workgroup would write its XCD's L2 back and drop what it holds of others' memory.
+template <int D>
+__device__ __forceinline__ void merge_here(const ChunkParams &p, const Piece &pc, const Req &rq, int first, int n, uint32_t *said, int tid)
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // this wavefront's rows are stored ...
+    __syncthreads();                                    // ... and all the workgroup's
+    if (tid == 0) {
+        u64 *count = &p.words[first & (MERGE_GROUPS - 1)].arrived[first / MERGE_GROUPS];
+        static_assert(MOST_TEAMS / MERGE_GROUPS <= 31, "a word for every block");
+        const bool last = __hip_atomic_fetch_add(count, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (u64)(n - 1);
+        if (last) __hip_atomic_store(count, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *said = last;
+    }
+    __syncthreads();
+    if (!*said) return;
+    const int x = tid >> 4, node = (x * p.ginv) >> 16, sub = tid & 15;
+    if (node >= pc.nodes) return;
+    join_parts<D, 1, true>(p, n, sub, [&](int i, int) { return (size_t)(first + i) * FEW_ROWS + x; }, [&](int, const auto &o) {
+        const size_t orow = (size_t)(rq.q0 + pc.node0 + node) * p.Hq + pc.g * p.G + (x - node * p.G);
+        *reinterpret_cast<std::decay_t<decltype(o)> *>(static_cast<__bf16 *>(p.O) + orow * D + sub * (D / 16)) = o;
+    });
+}
+
+template <int D, int RW, int KW, int NT, int EB>
+__global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams p)
+{
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    // (every argument in one round trip)
+    asm volatile("" ::"s"(p.Q), "s"(p.K), "s"(p.V), "s"(p.O), "s"(p.block_table), "s"(p.q_offset), "s"(p.prefix_len), "s"(p.Opart), "s"(p.ML), "s"(p.flag), "s"(p.M),
+                 "s"(p.L), "s"(p.Hq), "s"(p.Hkv), "s"(p.G), "s"(p.ginv), "s"(p.max_blocks), "s"(p.num_blocks), "s"(p.total_M), "s"(p.batch), "s"(p.wmin),
+                 "s"(p.scale_log2), "s"(p.out_scale), "s"(p.left), "s"(p.nb), "s"(p.inv_nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys), "s"(p.start), "s"(p.weight));
+    Chunk c;
+    Walk k = share_out(p, threadIdx.x & 63, blockIdx.x == 0 && threadIdx.x < 64, c);
+    using CL = ChunkLds<D, RW, KW, NT, EB>;
+    const uint32_t kept = (uint32_t)(uintptr_t)BTV_LDS_PTR(smem) + CL::PL::BYTES;
+    if (CL::KEPT && threadIdx.x < 64) keep_chunk(kept, threadIdx.x, c);     // (barriers before it is read: those of the first piece)
+    Left left = { 0, 0, 0, 0 };
+    for (bool again = false;; again = true) {
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));                   // keeps what derives from it (all addresses) from being carried across pieces
+        if (again) {
+            if (k.pos >= k.end) break;
+            c = CL::KEPT ? kept_chunk(kept, tid & 63) : load_chunk(p, 0, tid & 63, 0);
+        }
+        Piece pc = {};
+        Req rq = {};
+        int parts = 1, part = 0;
+        if (!(k.part ? only_piece(p, k, c, pc, rq, left, parts, part) : next_piece(p, k, tid & 63, c, pc, rq, left))) break;
+        attn_piece<D, RW, KW, NT, true, EB, true>(p, smem, tid, rq, pc, [] {});
+        // every wave is done with this piece's LDS, its own fills have landed; the stores may still be on their way
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        if constexpr (RW == 2)
+            if (p.words) {
+                if (parts > 1) merge_here<D>(p, pc, rq, k.team - part, parts, reinterpret_cast<uint32_t *>(smem), tid);
+                return;
+            }
+    }
+    if (threadIdx.x == 0 && !(RW == 2 && p.words)) p.left[k.team] = left;
+}
+
+// The blocks that were cut: 16 lanes per row, MERGE_ROWS rows per workgroup; workgroup (k, slice) looks at the block that share k has begun.
+constexpr int MERGE_ROWS = 32;
+template <int D>
+__global__ __launch_bounds__(256) void chunk_merge(ChunkParams p)
+{
+    asm volatile("" ::"s"(p.left), "s"(p.teams), "s"(p.wr), "s"(p.G), "s"(p.ginv), "s"(p.ML), "s"(p.Opart), "s"(p.O), "s"(p.Hq), "s"(p.out_scale));
+    const int k = blockIdx.x, lane = threadIdx.x & 63, sub = threadIdx.x & 15;
+    const Left left = p.left[k];
+    const int next = p.left[min(k + 1 + lane, p.teams - 1)].flags;
+    if (!(left.flags & BEGUN) || (int)blockIdx.y * MERGE_ROWS >= left.nodes * p.G) return;
+    // the first share behind k that ends a block ends this one (those between lie within it)
+    int n = 2;
+    unsigned long long ended = __builtin_amdgcn_ballot_w64(k + 1 + lane < p.teams && (next & ENDED));
+    for (int k0 = k + 1;;) {
+        if (ended) { n = k0 - k + __builtin_ctzll(ended) + 1; break; }
+        k0 += 64;
+        if (k0 >= p.teams) return;                      // (cannot be)
+        ended = __builtin_amdgcn_ballot_w64(k0 + lane < p.teams && (p.left[min(k0 + lane, p.teams - 1)].flags & ENDED));
+    }
+    const int x0 = blockIdx.y * MERGE_ROWS + (threadIdx.x >> 4);
+    join_parts<D, MERGE_ROWS / 16, false>(p, n, sub, [&](int i, int r) { return (size_t)(2 * (k + i) + (i == 0)) * p.wr + x0 + 16 * r; }, [&](int r, const auto &o) {
+        const int x = x0 + 16 * r, node = (x * p.ginv) >> 16;
+        if (node >= left.nodes) return;
+        const size_t orow = (size_t)(left.row0 + node) * p.Hq + left.g * p.G + (x - node * p.G);
+        *reinterpret_cast<std::decay_t<decltype(o)> *>(static_cast<__bf16 *>(p.O) + orow * D + sub * (D / 16)) = o;
+    });
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
@@ -425,12 +488,18 @@ bool cuts(int M_max, int L_max) { return (L_max + M_max + 31) / 32 > SMALL; }
 // What a row block costs besides its keys, in tiles of whole blocks: finding it, its first loads, its last steps and stores.
 int start_of(int wr, int D, int eb) { return wr == 64 ? 14 : eb == 1 ? 16 : D == 64 ? 12 : 9; }
 
+// Single tokens of few requests: parts of their keys that the workgroups merge themselves, up to two parts per place on the chip where there are few, four where the requests alone
+// may fill it.
+bool merges_inside(int batch, int M_max, int G, int Hkv) { return M_max * G <= FEW_ROWS && batch <= 64 && batch * Hkv <= 512; }
+int teams_inside(int batch, int Hkv) { return batch * Hkv <= 256 ? 512 : MOST_TEAMS; }
+
 struct WsLayout { size_t left, ml, opart, total; };
 WsLayout ws_layout(int wr, int D, bool cut)
 {
     WsLayout w;
     size_t off = BTV_WS_HEADER + MERGE_WORDS;
-    const size_t rows = cut ? (size_t)teams_of(wr) * 2 * wr : 0;
+    const size_t rows = cut ? (size_t)teams_of(wr) * 2 * wr : 0;        // (more than MOST_TEAMS * FEW_ROWS, which the parts of few rows take)
+    static_assert(512 * 2 * 64 >= MOST_TEAMS * FEW_ROWS, "parts of few rows have room where shares of 64 rows have");
     w.left = off; off += MOST_TEAMS * sizeof(Left);
     w.ml = off; off += rows * 16;
     w.opart = off; off += rows * D * 2;
@@ -499,6 +568,11 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     p.wmin = p.start + 8 * 32 * WHOLE;
     p.weight = (i64)M_max * G * 2 <= wr ? PART : WHOLE;
     p.most_keys = (int)std::min<i64>((i64)max_blocks * BTV_PAGE, INT_MAX);
+    const bool inside = merges_inside(batch, M_max, G, Hkv) && L_max + M_max < 1 << 25;        // (in a part's place tiles times parts stay in 32 bits)
+    if (inside) {
+        p.words = reinterpret_cast<MergeWords *>(w8 + BTV_WS_HEADER);
+        p.teams = teams_inside(batch, Hkv);
+    }
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define BTV_CASE(DD, EE, RR, KK, NN) if (D == DD && eb == EE && wr == RR * 32) rc = launch<DD, RR, KK, NN, EE>(p, st); else
     BTV_CASE(128, 2, 2, 2, 5) BTV_CASE(128, 2, 4, 2, 8) BTV_CASE(128, 2, 8, 1, 8)
@@ -506,7 +580,7 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     BTV_CASE(128, 1, 2, 2, 5) BTV_CASE(128, 1, 4, 2, 8)
     return btv_fail(BTV_EINVAL, "no kernel for D=%d", D);
 #undef BTV_CASE
-    if (rc || !cut) return rc;
+    if (rc || !cut || inside) return rc;
     const dim3 grid(p.teams, wr / MERGE_ROWS);
     if (D == 64) hipLaunchKernelGGL(chunk_merge<64>, grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL(chunk_merge<128>, grid, dim3(256), 0, st, p);

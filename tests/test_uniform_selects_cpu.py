@@ -17,20 +17,25 @@ SETS_SCC = re.compile(r"s_(add|sub|addc|subb|cmp|bitcmp|and|or|xor|andn2|orn2|na
 
 
 def unconnected(listing):
-    """(comparison, selection) pairs with nothing between them that sets the scalar condition."""
-    found, compared = [], None
+    """(comparison, selection) pairs with nothing between them that sets the scalar condition, where no scalar comparison ahead of them has set it for that selection."""
+    found, compared, meant = [], None, False
     for line in listing.splitlines():
         text = line.split("//")[0].strip()
         if not text or text.endswith(":"):
-            compared = None
+            compared, meant = None, False
             continue
         op = text.split()[0]
         if re.match(r"v_cmp_\w+_[iu]64", op):
             compared = text
-        elif op.startswith("s_cselect") and compared:
-            found.append((compared, text))
-        elif SETS_SCC.match(op) or op.startswith(("s_branch", "s_cbranch", "s_endpgm")):
-            compared = None
+        elif op.startswith("s_cselect"):
+            if compared and not meant:
+                found.append((compared, text))
+            elif not compared:
+                meant = False
+        elif SETS_SCC.match(op):
+            compared, meant = None, op.startswith(("s_cmp", "s_bitcmp"))
+        elif op.startswith(("s_branch", "s_cbranch", "s_endpgm")):
+            compared, meant = None, False
     return found
 
 
@@ -42,6 +47,7 @@ def test_the_check_sees_a_selection_without_its_comparison():
 """
     assert len(unconnected(bad)) == 1
     assert unconnected(bad.replace("	s_cselect", "	s_cmp_lg_u64 vcc, 0\n	s_cselect")) == []
+    assert unconnected(bad.replace("s_ashr_i32 s19, s18, 31", "s_cmp_lt_i32 s14, 7")) == []          # (a selection by that comparison)
 
 
 def test_no_selection_is_without_its_comparison(tmp_path):
