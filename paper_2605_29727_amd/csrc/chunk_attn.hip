@@ -11,7 +11,8 @@
 // the weight is WHOLE, or PART where no more than half of the block's rows exist and a tile goes faster); blocks lie one after the other, request
 // after request, KV head after KV head, and workgroup k takes what lies between k w and (k + 1) w.  Where that cuts a block, each part's rows go to the
 // workgroup's own place in the workspace (two at most: a block that it carries on with, one that it begins), and chunk_merge joins them in the order of the keys.
-// Neighbouring shares are on one XCD, which so keeps to one KV head or two, whose K/V its workgroups meet in their L2.
+// Neighbouring shares are on one XCD, which so keeps to one KV head or two, whose K/V its workgroups meet in their L2.  Where there are fewer blocks than workgroups, blocks go
+// in even parts instead, and where there are more, but a few for each workgroup at most and of lengths that come out even, whole blocks in turns.
 #include "attn_piece.h"
 
 #include <atomic>
@@ -91,7 +92,7 @@ __device__ __forceinline__ i64 lane_value(i64 x, int lane)
 }
 
 // 64 requests, one per lane, and where each ends in a KV head's work.
-struct Chunk { int q0, L, M; i64 incl; bool bad; };
+struct Chunk { int q0, L, M, beyond; i64 incl; bool bad; };      // (beyond: the order of whole blocks)
 __device__ __forceinline__ Chunk load_chunk(const ChunkParams &p, int c0, int lane, i64 before)
 {
     Chunk c;
@@ -108,8 +109,8 @@ __device__ __forceinline__ Chunk load_chunk(const ChunkParams &p, int c0, int la
     c.incl = wave_sums_of_lengths(c.M ? length_of(p, c.L, c.M) : 0) + before;
     return c;
 }
-// The first chunk is kept in LDS from one piece to the next (raw instructions: ahead of ordinary reads the compiler waits for the last piece's stores), but where
-// two workgroups fill the LDS of a CU to the last byte; there it is loaded again.
+// The first chunk is kept in LDS from one piece to the next, and where each wavefront stands (raw instructions: ahead of ordinary reads the compiler waits for the last
+// piece's stores, as it would for registers that it spills), but where two workgroups fill the LDS of a CU to the last byte; there the chunk is loaded again.
 constexpr int CHUNK_BYTES = 64 * 32;
 template <int D, int RW, int KW, int NT, int EB>
 struct ChunkLds {
@@ -117,27 +118,50 @@ struct ChunkLds {
     static constexpr bool KEPT = (PL::BYTES + CHUNK_BYTES) * PL::PER_CU <= 160 * 1024;
     static constexpr int BYTES = PL::BYTES + (KEPT ? CHUNK_BYTES : 0);
 };
-__device__ __forceinline__ void keep_chunk(uint32_t kept, int lane, const Chunk &c)
-{
-    asm volatile("ds_write_b64 %0, %1\n\tds_write2_b32 %0, %2, %3 offset0:2 offset1:3\n\tds_write_b32 %0, %4 offset:16\n\ts_waitcnt lgkmcnt(0)"
-                 :: "v"(kept + (uint32_t)lane * 32), "v"(c.incl), "v"(c.L), "v"(c.M), "v"(c.q0) : "memory");
-}
-__device__ __forceinline__ Chunk kept_chunk(uint32_t kept, int lane)
-{
-    Chunk c;
-    asm volatile("ds_read_b64 %0, %4\n\tds_read_b32 %1, %4 offset:8\n\tds_read_b32 %2, %4 offset:12\n\tds_read_b32 %3, %4 offset:16\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(c.incl), "=&v"(c.L), "=&v"(c.M), "=&v"(c.q0) : "v"(kept + (uint32_t)lane * 32) : "memory");
-    c.bad = false;
-    return c;
-}
-
 // Where a workgroup stands (every wavefront works it out for itself).
 struct Walk {
     i64 pos, end;                 // its share, and what comes next
     i64 head, wh;                 // where the current KV head's work begins; one head's work
     int h, team;                  // that head; the workgroup's place in the order of the shares
-    int part;                     // parts: tiles of a part (0: shares)
+    int part;                     // parts: tiles of a part (0: shares or whole blocks)
+    int step;                     // whole blocks: tiles of a step in their order (0: shares or parts); pos and end count turns
 };
+
+// Places of the lanes' numbers, one array after another, and of the wavefronts' walks.
+constexpr int WALK_BYTES = 64, AT_WALKS = CHUNK_BYTES - 8 * WALK_BYTES;
+__device__ __forceinline__ void keep_chunk(uint32_t kept, int lane, const Chunk &c)
+{
+    asm volatile("ds_write_b64 %0, %2\n\tds_write_b32 %1, %3 offset:512\n\tds_write_b32 %1, %4 offset:768\n\tds_write_b32 %1, %5 offset:1024\n\t"
+                 "ds_write_b32 %1, %6 offset:1280\n\ts_waitcnt lgkmcnt(0)"
+                 :: "v"(kept + (uint32_t)lane * 8), "v"(kept + (uint32_t)lane * 4), "v"(c.incl), "v"(c.L), "v"(c.M), "v"(c.q0), "v"(c.beyond) : "memory");
+}
+static_assert(AT_WALKS == 1536, "the offsets here");
+typedef int int4v __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void keep_walk(uint32_t kept, int tid, const Walk &k, const Left &left)
+{
+    const int4v a = { (int)k.pos, (int)(k.pos >> 32), (int)k.end, (int)(k.end >> 32) }, b = { (int)k.head, (int)(k.head >> 32), (int)k.wh, (int)(k.wh >> 32) };
+    const int4v c = { k.h, k.team, k.part, k.step }, d = { left.flags, left.row0, left.nodes, left.g };
+    if ((tid & 63) == 0)
+        asm volatile("ds_write_b128 %0, %1\n\tds_write_b128 %0, %2 offset:16\n\tds_write_b128 %0, %3 offset:32\n\tds_write_b128 %0, %4 offset:48\n\ts_waitcnt lgkmcnt(0)"
+                     :: "v"(kept + AT_WALKS + (tid >> 6) * WALK_BYTES), "v"(a), "v"(b), "v"(c), "v"(d) : "memory");
+}
+__device__ __forceinline__ Chunk kept_chunk(uint32_t kept, int tid, Walk &k, Left &left)
+{
+    Chunk c;
+    int4v w[4];
+    asm volatile("ds_read_b128 %0, %11\n\tds_read_b128 %1, %11 offset:16\n\tds_read_b128 %2, %11 offset:32\n\tds_read_b128 %3, %11 offset:48\n\t"
+                 "ds_read_b64 %4, %9\n\tds_read_b32 %5, %10 offset:512\n\tds_read_b32 %6, %10 offset:768\n\tds_read_b32 %7, %10 offset:1024\n\t"
+                 "ds_read_b32 %8, %10 offset:1280\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]), "=&v"(c.incl), "=&v"(c.L), "=&v"(c.M), "=&v"(c.q0), "=&v"(c.beyond)
+                 : "v"(kept + (uint32_t)(tid & 63) * 8), "v"(kept + (uint32_t)(tid & 63) * 4), "v"(kept + AT_WALKS + (tid >> 6) * WALK_BYTES) : "memory");
+    c.bad = false;
+    auto word = [&](int i) { return __builtin_amdgcn_readfirstlane(w[i >> 2][i & 3]); };
+    auto pair = [&](int i) { return (i64)(((unsigned long long)(uint32_t)word(i + 1) << 32) | (uint32_t)word(i)); };
+    k.pos = pair(0); k.end = pair(2); k.head = pair(4); k.wh = pair(6);
+    k.h = word(8); k.team = word(9); k.part = word(10); k.step = word(11);
+    left.flags = word(12); left.row0 = word(13); left.nodes = word(14); left.g = word(15);
+    return c;
+}
 
 // The place in the order of `active` shares on each XCD, neighbours on one XCD; the others have no work, but say so.
 __device__ __forceinline__ int team_of(int per_xcd)
@@ -157,7 +181,56 @@ __device__ __forceinline__ int divided(int n, int d, float inv)
 }
 __device__ __forceinline__ int parts_of(int t, int part, float inv) { return divided(t + part - 1, part, inv); }
 
-__device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool leader, Chunk &c)
+// The order of whole blocks: the longest first, of all requests, a block's KV heads beside each other.  Turn by turn the workgroups take one each, back and
+// forth, so that who had a long one has a short one next; eight neighbours stay in their order, and so on their XCD's KV heads.  Lengths count in 64 steps of
+// as many tiles: lane j knows how many blocks (of one KV head) are longer than j steps, and that gives a place in the order its step.
+// Shares are even, but each carries on with a block that another has begun, and cuts are merged: whole blocks may take MORE tiles longer (14 prompts of up to 615 tokens, 32 heads
+// of 64: 32 us in shares, 21 whole; 26 of up to 1096, 28 heads of 128: 103 and 93; a chunk of 2048 behind 30720, 64 heads: 1900 and 1820.  With 45 tiles more
+// 9 chunks of up to 1024 behind 2371 at most took 68 us whole and 62 in shares; with 14 the 26 prompts stayed in shares).
+constexpr int TURNS = 8, MORE = 28;
+__device__ __forceinline__ int unit_of(const ChunkParams &p, int team, int turn)
+{
+    return turn * p.teams + ((turn & 1) ? (p.teams - 8 - (team & ~7)) + (team & 7) : team);
+}
+// How many of a request's blocks are longer than t tiles: whole ones, and one of the rest.
+__device__ __forceinline__ int blocks_beyond(const ChunkParams &p, int L, int M, int t)
+{
+    const int keys = 32 * t + 1 - L;                    // new rows up to and with the last one of such a block, at least
+    const int whole = quotient(M, p.nb, p.inv_nb), first = quotient(max(keys, 1) + p.nb - 1, p.nb, p.inv_nb);
+    return max(whole - first + 1, 0) + (M > whole * p.nb && M >= keys);
+}
+__device__ __forceinline__ int step_at(int beyond, int rank) { return __builtin_popcountll(__builtin_amdgcn_ballot_w64(beyond > rank)) - 1; }    // -1: not as many blocks
+// Whether whole blocks take no longer than shares: what the first, the middle and the last workgroup have, against a share, a block that it carries on with and the merge.
+template <int WAVES>
+__device__ __forceinline__ bool whole_blocks(const ChunkParams &p, Walk &k, Chunk &c, int lane, int units, int longest, i64 w, int *counts)
+{
+    const int most_length = (int)least(w + MORE * 32 * WHOLE, INT_MAX);
+    k.step = (longest + 63) >> 6;
+    if (longest * (32 * WHOLE) > most_length) return false;
+    int n = 0;                                          // the wavefronts share the requests out
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int r = wave; r < p.batch; r += WAVES) n += blocks_beyond(p, __builtin_amdgcn_readlane(c.L, r), __builtin_amdgcn_readlane(c.M, r), lane * k.step);
+    counts[wave * 64 + lane] = n;
+    __syncthreads();
+    c.beyond = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) c.beyond += counts[i * 64 + lane];
+    __syncthreads();                                    // (the first fills go there)
+    int most_sum = 0;
+    for (int s = 0; s < 3; ++s) {
+        const int team = s == 0 ? 0 : s == 1 ? p.teams >> 1 : p.teams - 1;
+        int sum = 0;
+        for (int turn = 0; turn * p.teams < units; ++turn) {
+            const int step = step_at(c.beyond, quotient(unit_of(p, team, turn), p.Hkv, p.inv_Hkv));
+            if (step >= 0) sum += p.start + (step * k.step + ((k.step + 1) >> 1)) * (32 * WHOLE);
+        }
+        most_sum = max(most_sum, sum);
+    }
+    return most_sum <= most_length;
+}
+
+template <bool FEW, int WAVES>
+__device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool leader, Chunk &c, int *counts)
 {
     Walk k;
     i64 all = 0;
@@ -168,7 +241,7 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
         all += lane_value(c.incl, 63);
     }
     if (leader && bad) atomicOr(p.flag, 2u);
-    k.head = 0; k.h = 0; k.part = 0;
+    k.head = 0; k.h = 0; k.part = 0; k.step = 0; c.beyond = 0;
     k.wh = all;
     all *= p.Hkv;
     const int teams_log2 = 31 - __builtin_clz(p.teams);
@@ -178,9 +251,16 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
         // many parts as its last).  A share costs its length and START for what it carries on with, a part its tiles and START: where requests differ so
         // much that the longest part takes longer, shares it is.
         const int blocks = quotient(c.M + p.nb - 1, p.nb, p.inv_nb), t = c.M ? (c.L + c.M + 31) >> 5 : 0;
-        const int all_blocks = __builtin_amdgcn_readlane(wave_sums(blocks), 63) * p.Hkv;
+        const int head_blocks = __builtin_amdgcn_readlane(wave_sums(blocks), 63), all_blocks = head_blocks * p.Hkv, longest = wave_max(t);
+        if constexpr (!FEW)
+            if (all_blocks > p.teams && all_blocks <= TURNS * p.teams && longest > SMALL && longest < 1 << 16
+                && whole_blocks<WAVES>(p, k, c, lane, all_blocks, longest, w, counts)) {
+                k.team = blockIdx.x;
+                k.pos = 0; k.end = (all_blocks + p.teams - 1) >> teams_log2;
+                return k;
+            }
+        k.step = 0;
         if (all_blocks <= p.teams && all_blocks > 0) {
-            const int longest = wave_max(t);
             // (not below what the work comes to for each, rounded down)
             int lo = max(LEAST_PART, (int)((float)(all - (i64)all_blocks * p.start) * (0.999f / 32) / (float)(p.weight * p.teams))), n = all_blocks;
             // what parts save has to be worth their merge
@@ -211,6 +291,23 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
     k.pos = least(k.team * w, all);
     k.end = least(k.pos + w, all);
     return k;
+}
+
+// The whole block of the next turn.
+__device__ __forceinline__ bool whole_piece(const ChunkParams &p, Walk &k, const Chunk &c, Piece &pc, Req &rq)
+{
+    const int unit = unit_of(p, k.team, (int)k.pos), rank = quotient(unit, p.Hkv, p.inv_Hkv), step = step_at(c.beyond, rank);
+    ++k.pos;
+    if (step < 0) { k.pos = k.end; return false; }      // (only the last turn is not full)
+    // of the blocks of this step, the requests' in turn
+    const int from = blocks_beyond(p, c.L, c.M, step * k.step), longer = step == 63 ? 0 : blocks_beyond(p, c.L, c.M, (step + 1) * k.step), upto = wave_sums(from - longer);
+    const int y = rank - __builtin_amdgcn_readlane(wave_sums(longer), 63), src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(y < upto));
+    rq.q0 = __builtin_amdgcn_readlane(c.q0, src); rq.L = __builtin_amdgcn_readlane(c.L, src); rq.M = __builtin_amdgcn_readlane(c.M, src);
+    const int i = y - __builtin_amdgcn_readlane(upto - (from - longer), src);
+    const int b = quotient(rq.M + p.nb - 1, p.nb, p.inv_nb) - __builtin_amdgcn_readlane(from, src) + i;
+    pc.rq = src; pc.g = unit - rank * p.Hkv; pc.by = b; pc.bx = 0; pc.node0 = b * p.nb; pc.nodes = min(p.nb, rq.M - pc.node0);
+    pc.st0 = 0; pc.st1 = (rq.L + pc.node0 + pc.nodes + 31) >> 5; pc.direct = 1;
+    return true;
 }
 
 // The only piece of a workgroup in the form of parts: part i of n of a block's tiles, cut behind even numbers of them (a round of two waves).
@@ -402,35 +499,46 @@ __global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams
     // (every argument in one round trip)
     asm volatile("" ::"s"(p.Q), "s"(p.K), "s"(p.V), "s"(p.O), "s"(p.block_table), "s"(p.q_offset), "s"(p.prefix_len), "s"(p.Opart), "s"(p.ML), "s"(p.flag), "s"(p.M),
                  "s"(p.L), "s"(p.Hq), "s"(p.Hkv), "s"(p.G), "s"(p.ginv), "s"(p.max_blocks), "s"(p.num_blocks), "s"(p.total_M), "s"(p.batch), "s"(p.wmin),
-                 "s"(p.scale_log2), "s"(p.out_scale), "s"(p.left), "s"(p.nb), "s"(p.inv_nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys), "s"(p.start), "s"(p.weight));
+                 "s"(p.scale_log2), "s"(p.out_scale), "s"(p.left), "s"(p.nb), "s"(p.inv_nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys), "s"(p.start), "s"(p.weight), "s"(p.inv_Hkv), "s"(p.words));
     Chunk c;
-    Walk k = share_out(p, threadIdx.x & 63, blockIdx.x == 0 && threadIdx.x < 64, c);
+    Walk k = share_out<RW == 2, RW * KW>(p, threadIdx.x & 63, blockIdx.x == 0 && threadIdx.x < 64, c, reinterpret_cast<int *>(smem));
     using CL = ChunkLds<D, RW, KW, NT, EB>;
     const uint32_t kept = (uint32_t)(uintptr_t)BTV_LDS_PTR(smem) + CL::PL::BYTES;
+    static_assert(CL::PL::BYTES % 16 == 0 && RW * KW <= 8, "what is kept");
+    static_assert(RW == 2 || CL::KEPT, "the turns of whole blocks");
     if (CL::KEPT && threadIdx.x < 64) keep_chunk(kept, threadIdx.x, c);     // (barriers before it is read: those of the first piece)
     Left left = { 0, 0, 0, 0 };
     for (bool again = false;; again = true) {
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));                   // keeps what derives from it (all addresses) from being carried across pieces
         if (again) {
-            if (k.pos >= k.end) break;
-            c = CL::KEPT ? kept_chunk(kept, tid & 63) : load_chunk(p, 0, tid & 63, 0);
+            if constexpr (CL::KEPT) c = kept_chunk(kept, tid, k, left);
+            else c = load_chunk(p, 0, tid & 63, 0);
         }
         Piece pc = {};
         Req rq = {};
         int parts = 1, part = 0;
-        if (!(k.part ? only_piece(p, k, c, pc, rq, left, parts, part) : next_piece(p, k, tid & 63, c, pc, rq, left))) break;
+        bool more;
+        if (RW != 2 && k.step) more = whole_piece(p, k, c, pc, rq);
+        else if (k.part) more = only_piece(p, k, c, pc, rq, left, parts, part);
+        else more = next_piece(p, k, tid & 63, c, pc, rq, left);
+        const bool last = k.pos >= k.end;
+        if (!more || last) {
+            if (tid == 0 && !(RW == 2 && p.words)) p.left[k.team] = left;
+            if (!more) return;
+        } else if constexpr (CL::KEPT) keep_walk(kept, tid, k, left);
         attn_piece<D, RW, KW, NT, true, EB, true>(p, smem, tid, rq, pc, [] {});
+        if constexpr (RW == 2)
+            if (parts > 1 && p.words) {
+                // every wave is done with this piece's LDS
+                merge_here<D>(p, pc, rq, k.team - part, parts, reinterpret_cast<uint32_t *>(smem), tid);
+                return;
+            }
+        if (last) return;
         // every wave is done with this piece's LDS, its own fills have landed; the stores may still be on their way
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
-        if constexpr (RW == 2)
-            if (p.words) {
-                if (parts > 1) merge_here<D>(p, pc, rq, k.team - part, parts, reinterpret_cast<uint32_t *>(smem), tid);
-                return;
-            }
     }
-    if (threadIdx.x == 0 && !(RW == 2 && p.words)) p.left[k.team] = left;
 }
 
 // The blocks that were cut: 16 lanes per row, MERGE_ROWS rows per workgroup; workgroup (k, slice) looks at the block that share k has begun.
@@ -560,6 +668,7 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     p.ML = reinterpret_cast<float *>(w8 + wl.ml);
     p.flag = reinterpret_cast<uint32_t *>(w8);
     p.M = M_max; p.L = L_max; p.Hq = Hq; p.Hkv = Hkv; p.G = G; p.ginv = (65536 + G - 1) / G;
+    p.inv_Hkv = reciprocal(Hkv);
     p.max_blocks = max_blocks; p.num_blocks = num_blocks; p.total_M = total_M; p.batch = batch;
     p.scale_log2 = factor; p.out_scale = v_scale;
     p.left = reinterpret_cast<Left *>(w8 + wl.left);

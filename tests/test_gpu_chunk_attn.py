@@ -123,6 +123,16 @@ def test_work_for_all_workgroups(kv, Hq, Hkv, D, Ls, Ms):
     check(b, run(b))
 
 
+# More row blocks than workgroups, by little and by up to eight times, of lengths that whole blocks share out evenly and of others; head counts that do and do not divide the chip.
+@pytest.mark.parametrize("kv,Hq,Hkv,D", [("bf16", 16, 8, 128), ("bf16", 32, 8, 64), ("fp8", 8, 8, 128), ("bf16", 24, 6, 128), ("bf16", 12, 12, 64), ("fp8", 7, 7, 128)])
+@pytest.mark.parametrize("Ls,Ms", [([0], [4300]), ([3000], [4096]), ([0, 0, 0, 0], [1600, 2000, 1, 1111]), ([5, 900, 0, 0, 77, 3, 40, 2000], [1800, 0, 700, 129, 1000, 65, 1500, 333]),
+                                   ([20000, 0], [700, 3500]),
+                                   ([0, 9, 64] * 20, [400, 33, 170] * 20)], ids=lambda x: "-".join(map(str, x[:8])))
+def test_more_blocks_than_workgroups(kv, Hq, Hkv, D, Ls, Ms):
+    b = make(3 * sum(Ls) + sum(Ms), Ls, Ms, Hq, Hkv, D, kv)
+    check(b, run(b))
+
+
 @pytest.mark.parametrize("kv,Hq,Hkv,D", SHAPES, ids=SHAPE_IDS)
 @pytest.mark.parametrize("Ls,Ms", [([10, 0, 700, 33], [1, 1, 1, 1]), ([0, 100, 50], [40, 0, 7]), ([0, 4000, 17, 900], [500, 1, 64, 130]), ([0, 0, 0], [300, 1, 77]),
                                    ([7, 12000, 3], [0, 3, 0]), ([40, 6000, 1, 300, 2000], [33, 1, 257, 16, 65])], ids=lambda x: "-".join(map(str, x)))
