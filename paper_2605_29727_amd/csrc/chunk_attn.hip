@@ -584,11 +584,26 @@ int check_chunk(int batch, int M_max, int L_max, int Hq, int Hkv, int D)
     return BTV_OK;
 }
 
-// Rows per workgroup by the largest request's packed rows.
-int rows_per_block(int M_max, int G, int eb)
+// Rows per workgroup: at most what the largest request has.
+int most_rows(int M_max, int G, int eb)
 {
     const i64 rows = (i64)M_max * G;
     return rows <= 64 ? 64 : rows <= 128 || eb == 1 ? 128 : 256;
+}
+// Many rows read a tile for more of them and are the fastest over long ranges (a chunk of 2048 behind 30720, 64 heads of 128: 256 rows 1834 us, 128 2055), but where they leave
+// workgroups without a block, or one in a second turn, the ends of the pieces are most of the time: fewer rows then, as long as the work is short.  By the numbers of
+// blocks that the bounds allow (half a block of each request is not full) and the tiles of 256 rows that come to each workgroup.  us with 256, 128, 64 rows:
+// 7 prompts of up to 718, 8 heads of 64: 23.3, 16.5, 13.8 (93 blocks of 256 rows, 4 tiles); 7 chunks of up to 215 behind 1598, 64 heads of 128: 42.7, 27.2, 42.1
+// (165, 34); 2 prompts of up to 3676, 32 heads of 64: 34.2, 36.5, 44.5 (284, 64); 5 chunks of up to 749 behind 12384, 32 heads of 128: 110, 120, 171 (115, 179);
+// E4M3, a chunk of 1938, 8 heads: 16.3 with 128, 12.8 with 64 (10, 1); 22 of up to 110 behind 8711: 34.2, 36.2 (45, 48).
+int rows_per_block(int batch, int total_M, int M_max, int L_max, int G, int Hkv, int eb)
+{
+    const int most = most_rows(M_max, G, eb);
+    const double rows = (double)total_M * G, half = 0.5 * batch;
+    const double tiles = (rows / 256 + half) * Hkv * ((double)L_max + 0.5 * M_max) / (32 * 256);
+    if ((rows / 64 + half) * Hkv <= 512 && tiles <= 30) return 64;
+    if ((rows / 256 + half) * Hkv <= 256 && tiles <= 110) return std::min(most, 128);
+    return most;
 }
 int teams_of(int wr) { return wr == 64 ? 512 : 256; }           // one workgroup per CU, or two of the small ones
 bool cuts(int M_max, int L_max) { return (L_max + M_max + 31) / 32 > SMALL; }
@@ -618,7 +633,7 @@ size_t enough_for(int M_max, int L_max, int G, int D, int eb)
 {
     const bool cut = cuts(M_max, L_max);
     size_t most = 0;
-    for (int wr = 64; wr <= rows_per_block(M_max, G, eb); wr *= 2) most = std::max(most, ws_layout(wr, D, cut).total);
+    for (int wr = 64; wr <= most_rows(M_max, G, eb); wr *= 2) most = std::max(most, ws_layout(wr, D, cut).total);
     return most;
 }
 
@@ -654,7 +669,7 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     BTV_REQUIRE(std::isfinite(scale) && std::fabs(scale) <= 1e30f, "the scale must be finite");
     const float factor = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) * k_scale * 1.4426950408889634f;
     BTV_REQUIRE(std::isfinite(factor) && factor > 0.f, "the scale must be finite");
-    const int G = Hq / Hkv, wr = rows_per_block(M_max, G, eb);
+    const int G = Hq / Hkv, wr = rows_per_block(batch, total_M, M_max, L_max, G, Hkv, eb);
     const bool cut = cuts(M_max, L_max);
     const WsLayout wl = ws_layout(wr, D, cut);
     rc = btv_check_ws(ws, ws_bytes, wl.total);

@@ -171,6 +171,18 @@ def test_other_scales_and_bounds_above_the_lengths(kv, Hq, Hkv, D):
     check(b, run(b, scale=0.001, M_max=1000, L_max=320), scale=0.001)
 
 
+# Bounds far above the lengths, as a captured call has them, ask for the most rows per workgroup whatever the requests are.
+@pytest.mark.parametrize("kv,Hq,Hkv,D", SHAPES, ids=SHAPE_IDS)
+@pytest.mark.parametrize("Ls,Ms", [([0], [1]), ([37], [1]), ([15], [2]), ([31], [40]), ([0], [64]), ([63], [65]), ([5], [200]), ([96], [97]), ([159], [1]), ([255], [9]), ([290], [3]),
+                                   ([0], [257]), ([60], [229]), ([3000], [1]), ([9000], [17]), ([2500], [300]), ([10, 0, 700, 33], [1, 1, 1, 1]), ([0, 4000, 17, 900], [500, 1, 64, 130]),
+                                   ([7, 12000, 3], [0, 3, 0]), ([40, 6000, 1, 300, 2000], [33, 1, 257, 16, 65])], ids=lambda x: "-".join(map(str, x)))
+def test_bounds_for_the_most_rows(kv, Hq, Hkv, D, Ls, Ms):
+    import torch
+    b = make(sum(Ls) + 5 * sum(Ms), Ls, Ms, Hq, Hkv, D, kv)
+    b["table"] = torch.nn.functional.pad(b["table"], (0, 1_000_016 // PAGE - b["table"].shape[1]), value=-5)
+    check(b, run(b, M_max=2000, L_max=1_000_000))
+
+
 @pytest.mark.parametrize("Ms", [[3, 40], [200, 300]], ids=["few", "many"])
 def test_rows_that_nobody_owns_stay(Ms):
     b = make(6, [100, 0], Ms, 8, 2, 128, "bf16", pad=9)
