@@ -596,16 +596,24 @@ int most_rows(int M_max, int G, int eb)
 // 7 prompts of up to 718, 8 heads of 64: 23.3, 16.5, 13.8 (93 blocks of 256 rows, 4 tiles); 7 chunks of up to 215 behind 1598, 64 heads of 128: 42.7, 27.2, 42.1
 // (165, 34); 2 prompts of up to 3676, 32 heads of 64: 34.2, 36.5, 44.5 (284, 64); 5 chunks of up to 749 behind 12384, 32 heads of 128: 110, 120, 171 (115, 179);
 // E4M3, a chunk of 1938, 8 heads: 16.3 with 128, 12.8 with 64 (10, 1); 22 of up to 110 behind 8711: 34.2, 36.2 (45, 48).
-int rows_per_block(int batch, int total_M, int M_max, int L_max, int G, int Hkv, int eb)
+// With 64 channels two workgroups of 128 rows, four waves that take every tile, fit on a CU: of many blocks one's ends pass while the other computes, but each brings its own
+// tiles.  us with 256 rows and so: 6 prompts of up to 2348, 16 heads: 41.7, 34.9 (396 blocks, 57 tiles); 26 of up to 125, 32 heads: 17.6, 9.0 (258, 2); 34 chunks of up to
+// 545 behind 4275, 16 heads: 65.2, 65.6 (454, 252); 7 of up to 551 behind 25259, 16 heads: 70.2, 76.8 (141, 440).
+struct Shape { int rows, key_waves, teams; };
+Shape shape_of(int batch, int total_M, int M_max, int L_max, int G, int Hkv, int D, int eb)
 {
     const int most = most_rows(M_max, G, eb);
     const double rows = (double)total_M * G, half = 0.5 * batch;
     const double tiles = (rows / 256 + half) * Hkv * ((double)L_max + 0.5 * M_max) / (32 * 256);
-    if ((rows / 64 + half) * Hkv <= 512 && tiles <= 30) return 64;
-    if ((rows / 256 + half) * Hkv <= 256 && tiles <= 110) return std::min(most, 128);
-    return most;
+    if ((rows / 64 + half) * Hkv <= 512 && tiles <= 30) return { 64, 2, 512 };
+    if (most <= 64) return { 64, 2, 512 };
+    // (very short ones: a second turn costs as much as the first; 37 prompts of up to 234, 16 heads of 128: 15.4 with 256 rows, 22.9 with 128; 8 of up to 479, 32 heads, where
+    // 7 tiles come to each: 26.2, 22.3)
+    const bool few = (rows / 256 + half) * Hkv <= 256 && (tiles >= 4 || (rows / 128 + half) * Hkv <= 256);
+    if (most == 128 || (few && tiles <= 110)) return { 128, 2, 256 };
+    if (D == 64 && !few && tiles <= 200) return { 128, 1, 512 };
+    return { 256, 1, 256 };
 }
-int teams_of(int wr) { return wr == 64 ? 512 : 256; }           // one workgroup per CU, or two of the small ones
 bool cuts(int M_max, int L_max) { return (L_max + M_max + 31) / 32 > SMALL; }
 
 // What a row block costs besides its keys, in tiles of whole blocks: finding it, its first loads, its last steps and stores.
@@ -617,11 +625,11 @@ bool merges_inside(int batch, int M_max, int G, int Hkv) { return M_max * G <= F
 int teams_inside(int batch, int Hkv) { return batch * Hkv <= 256 ? 512 : MOST_TEAMS; }
 
 struct WsLayout { size_t left, ml, opart, total; };
-WsLayout ws_layout(int wr, int D, bool cut)
+WsLayout ws_layout(int block_rows, int D, bool cut)
 {
     WsLayout w;
     size_t off = BTV_WS_HEADER + MERGE_WORDS;
-    const size_t rows = cut ? (size_t)teams_of(wr) * 2 * wr : 0;        // (more than MOST_TEAMS * FEW_ROWS, which the parts of few rows take)
+    const size_t rows = cut ? (size_t)block_rows * 2 : 0;               // (of all workgroups; more than MOST_TEAMS * FEW_ROWS, which the parts of few rows take)
     static_assert(512 * 2 * 64 >= MOST_TEAMS * FEW_ROWS, "parts of few rows have room where shares of 64 rows have");
     w.left = off; off += MOST_TEAMS * sizeof(Left);
     w.ml = off; off += rows * 16;
@@ -631,10 +639,7 @@ WsLayout ws_layout(int wr, int D, bool cut)
 }
 size_t enough_for(int M_max, int L_max, int G, int D, int eb)
 {
-    const bool cut = cuts(M_max, L_max);
-    size_t most = 0;
-    for (int wr = 64; wr <= most_rows(M_max, G, eb); wr *= 2) most = std::max(most, ws_layout(wr, D, cut).total);
-    return most;
+    return ws_layout(most_rows(M_max, G, eb) > 128 ? 256 * 256 : 256 * 128, D, cuts(M_max, L_max)).total;
 }
 
 template <int D, int RW, int KW, int NT, int EB>
@@ -669,9 +674,11 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     BTV_REQUIRE(std::isfinite(scale) && std::fabs(scale) <= 1e30f, "the scale must be finite");
     const float factor = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) * k_scale * 1.4426950408889634f;
     BTV_REQUIRE(std::isfinite(factor) && factor > 0.f, "the scale must be finite");
-    const int G = Hq / Hkv, wr = rows_per_block(batch, total_M, M_max, L_max, G, Hkv, eb);
+    const int G = Hq / Hkv;
+    const Shape sh = shape_of(batch, total_M, M_max, L_max, G, Hkv, D, eb);
+    const int wr = sh.rows;
     const bool cut = cuts(M_max, L_max);
-    const WsLayout wl = ws_layout(wr, D, cut);
+    const WsLayout wl = ws_layout(sh.teams * wr, D, cut);
     rc = btv_check_ws(ws, ws_bytes, wl.total);
     if (rc) return rc;
     if (total_M == 0) return BTV_OK;
@@ -687,7 +694,7 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     p.max_blocks = max_blocks; p.num_blocks = num_blocks; p.total_M = total_M; p.batch = batch;
     p.scale_log2 = factor; p.out_scale = v_scale;
     p.left = reinterpret_cast<Left *>(w8 + wl.left);
-    p.wr = wr; p.nb = wr / G; p.inv_nb = reciprocal(p.nb); p.teams = teams_of(wr);
+    p.wr = wr; p.nb = wr / G; p.inv_nb = reciprocal(p.nb); p.teams = sh.teams;
     p.start = start_of(wr, D, eb) * 32 * WHOLE;
     p.wmin = p.start + 8 * 32 * WHOLE;
     p.weight = (i64)M_max * G * 2 <= wr ? PART : WHOLE;
@@ -698,9 +705,9 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
         p.teams = teams_inside(batch, Hkv);
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
-#define BTV_CASE(DD, EE, RR, KK, NN) if (D == DD && eb == EE && wr == RR * 32) rc = launch<DD, RR, KK, NN, EE>(p, st); else
+#define BTV_CASE(DD, EE, RR, KK, NN) if (D == DD && eb == EE && wr == RR * 32 && sh.key_waves == KK) rc = launch<DD, RR, KK, NN, EE>(p, st); else
     BTV_CASE(128, 2, 2, 2, 5) BTV_CASE(128, 2, 4, 2, 8) BTV_CASE(128, 2, 8, 1, 8)
-    BTV_CASE(64, 2, 2, 2, 5) BTV_CASE(64, 2, 4, 2, 8) BTV_CASE(64, 2, 8, 1, 8)
+    BTV_CASE(64, 2, 2, 2, 5) BTV_CASE(64, 2, 4, 2, 8) BTV_CASE(64, 2, 4, 1, 8) BTV_CASE(64, 2, 8, 1, 8)
     BTV_CASE(128, 1, 2, 2, 5) BTV_CASE(128, 1, 4, 2, 8)
     return btv_fail(BTV_EINVAL, "no kernel for D=%d", D);
 #undef BTV_CASE
