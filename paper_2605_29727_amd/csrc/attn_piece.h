@@ -908,7 +908,6 @@ struct Piece {
     // chunks only
     int node0, nodes;             // the row block's nodes
     int prow0;                    // where its partial's rows begin
-    bool through;                 // whether they are stored past this XCD's caches
 };
 
 // A page window (32 tiles' page ids) per 256 bytes, four of them in turn, behind everything else; not where two workgroups
@@ -1627,24 +1626,24 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
             const h2 lo = { (_Float16)fin[dt][q * 4 + 0], (_Float16)fin[dt][q * 4 + 1] }, hi = { (_Float16)fin[dt][q * 4 + 2], (_Float16)fin[dt][q * 4 + 3] };
             return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
         };
-        if constexpr (CAUSAL && RW == 2)
-            if (pc_.through) {
-                // (few rows, within the first 2^31 bytes)
-                const auto rows = __builtin_amdgcn_make_buffer_rsrc(p.Opart, 0, 0x7FFFFFFF, 0x00027000), ml = __builtin_amdgcn_make_buffer_rsrc(p.ML, 0, 0x7FFFFFFF, 0x00027000);
+        if constexpr (CAUSAL) {
+            // past this XCD's caches: a workgroup elsewhere may merge them (all parts lie within 2^31 bytes)
+            const auto rows = __builtin_amdgcn_make_buffer_rsrc(p.Opart, 0, 0x7FFFFFFF, 0x00027000), ml = __builtin_amdgcn_make_buffer_rsrc(p.ML, 0, 0x7FFFFFFF, 0x00027000);
 #pragma unroll
-                for (int dt = 0; dt < DTK; ++dt)
+            for (int dt = 0; dt < DTK; ++dt)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint2 a = pack(dt, q);
-                        const u32x2 w = { a.x, a.y };
-                        __builtin_amdgcn_raw_buffer_store_b64(w, rows, (int)((prow * D + (dt0 + dt) * 32 + 8 * q + 4 * h) * 2), 0, COHERENT);
-                    }
-                if (h == 0 && kw == 0) {
-                    const u32x4 w = { __float_as_uint(m_run), __float_as_uint(l_run), __float_as_uint(amax), 0u };
-                    __builtin_amdgcn_raw_buffer_store_b128(w, ml, (int)(prow * 16), 0, COHERENT);
+                for (int q = 0; q < 4; q += 2) {
+                    const uint2 a = pack(dt, q), b = pack(dt, q + 1);
+                    const auto x = __builtin_amdgcn_permlane32_swap(a.x, b.x, false, false), y = __builtin_amdgcn_permlane32_swap(a.y, b.y, false, false);
+                    const u32x4 w = { (uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1] };
+                    __builtin_amdgcn_raw_buffer_store_b128(w, rows, (int)((prow * D + (dt0 + dt) * 32 + (q + h) * 8) * 2), 0, COHERENT);
                 }
-                return;
+            if (h == 0 && kw == 0) {
+                const u32x4 w = { __float_as_uint(m_run), __float_as_uint(l_run), __float_as_uint(amax), 0u };
+                __builtin_amdgcn_raw_buffer_store_b128(w, ml, (int)(prow * 16), 0, COHERENT);
             }
+            return;
+        }
         store_rows(reinterpret_cast<unsigned char *>(p.Opart) + (prow * D + dt0 * 32) * 2, pack);
         if (h == 0 && kw == 0) *reinterpret_cast<float4 *>(p.ML + prow * 4) = make_float4(m_run, l_run, amax, 0.f);
     }

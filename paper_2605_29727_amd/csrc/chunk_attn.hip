@@ -10,7 +10,7 @@
 // The host knows bounds on the lengths only, so the workgroups share the work out themselves.  A row block is START + weight * keys long (the keys that its last node sees;
 // the weight is WHOLE, or PART where no more than half of the block's rows exist and a tile goes faster); blocks lie one after the other, request
 // after request, KV head after KV head, and workgroup k takes what lies between k w and (k + 1) w.  Where that cuts a block, each part's rows go to the
-// workgroup's own place in the workspace (two at most: a block that it carries on with, one that it begins), and chunk_merge joins them in the order of the keys.
+// workgroup's own place in the workspace (two at most: a block that it carries on with, one that it begins), and the workgroup that stores the last of them joins them in the order of the keys.
 // Neighbouring shares are on one XCD, which so keeps to one KV head or two, whose K/V its workgroups meet in their L2.  Where there are fewer blocks than workgroups, blocks go
 // in even parts instead, and where there are more, but a few for each workgroup at most and of lengths that come out even, whole blocks in turns.
 #include "attn_piece.h"
@@ -26,15 +26,9 @@ constexpr int WHOLE = 3, PART = 2;                              // weights of a 
 constexpr int MARGIN = 2, SMALL = 8;                            // tiles: a cut nearer to a block's ends moves there; blocks of up to SMALL are not cut
 constexpr int LEAST_PART = 4;                                   // tiles of the smallest part
 constexpr int MOST_ROWS = 1 << 20, MOST_TEAMS = 1024;
-constexpr int FEW_ROWS = 16;                                   // of a block whose parts the workgroups merge themselves
-
-// What a workgroup leaves for the merge: whether it has begun a block that others carry on with (and where that one's rows are), and whether the block
-// that it carried on with ends with its part.
-struct Left { int flags, row0, nodes, g; };                     // row0: the block's first row of Q and O as [total_M]
-constexpr int BEGUN = 1, ENDED = 2;
+constexpr int FEW_ROWS = 16;                                   // of single tokens' blocks, whose parts have less room
 
 struct ChunkParams : AttnParams {
-    Left *left;                   // [teams]
     int nb;                       // nodes per row block
     uint32_t inv_nb;              // for quotient()
     int wr;                       // rows per row block
@@ -42,7 +36,9 @@ struct ChunkParams : AttnParams {
     int start;                    // what a row block costs besides its keys
     int most_keys;                // what a row of the block table has room for
     int weight;                   // of a key, for the largest request's blocks
-    MergeWords *words;            // parts always, merged by the workgroup that stores the last of a block's (null: by a launch of its own)
+    int part_rows;                // a workgroup's room for a part's rows
+    MergeWords *words;            // how many of a block's parts are stored
+    int always_parts;             // few rows: parts whatever the shares would be
 };
 
 // 64-bit minimum and maximum of numbers less than 2^62 apart, by the sign of their difference.  (Of values that a wavefront has in common the compiler makes a vector
@@ -122,6 +118,7 @@ struct ChunkLds {
 struct Walk {
     i64 pos, end;                 // its share, and what comes next
     i64 head, wh;                 // where the current KV head's work begins; one head's work
+    i64 w;                        // a share
     int h, team;                  // that head; the workgroup's place in the order of the shares
     int part;                     // parts: tiles of a part (0: shares or whole blocks)
     int step;                     // whole blocks: tiles of a step in their order (0: shares or parts); pos and end count turns
@@ -137,15 +134,15 @@ __device__ __forceinline__ void keep_chunk(uint32_t kept, int lane, const Chunk 
 }
 static_assert(AT_WALKS == 1536, "the offsets here");
 typedef int int4v __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void keep_walk(uint32_t kept, int tid, const Walk &k, const Left &left)
+__device__ __forceinline__ void keep_walk(uint32_t kept, int tid, const Walk &k)
 {
     const int4v a = { (int)k.pos, (int)(k.pos >> 32), (int)k.end, (int)(k.end >> 32) }, b = { (int)k.head, (int)(k.head >> 32), (int)k.wh, (int)(k.wh >> 32) };
-    const int4v c = { k.h, k.team, k.part, k.step }, d = { left.flags, left.row0, left.nodes, left.g };
+    const int4v c = { k.h, k.team, k.part, k.step }, d = { (int)k.w, (int)(k.w >> 32), 0, 0 };
     if ((tid & 63) == 0)
         asm volatile("ds_write_b128 %0, %1\n\tds_write_b128 %0, %2 offset:16\n\tds_write_b128 %0, %3 offset:32\n\tds_write_b128 %0, %4 offset:48\n\ts_waitcnt lgkmcnt(0)"
                      :: "v"(kept + AT_WALKS + (tid >> 6) * WALK_BYTES), "v"(a), "v"(b), "v"(c), "v"(d) : "memory");
 }
-__device__ __forceinline__ Chunk kept_chunk(uint32_t kept, int tid, Walk &k, Left &left)
+__device__ __forceinline__ Chunk kept_chunk(uint32_t kept, int tid, Walk &k)
 {
     Chunk c;
     int4v w[4];
@@ -157,9 +154,8 @@ __device__ __forceinline__ Chunk kept_chunk(uint32_t kept, int tid, Walk &k, Lef
     c.bad = false;
     auto word = [&](int i) { return __builtin_amdgcn_readfirstlane(w[i >> 2][i & 3]); };
     auto pair = [&](int i) { return (i64)(((unsigned long long)(uint32_t)word(i + 1) << 32) | (uint32_t)word(i)); };
-    k.pos = pair(0); k.end = pair(2); k.head = pair(4); k.wh = pair(6);
+    k.pos = pair(0); k.end = pair(2); k.head = pair(4); k.wh = pair(6); k.w = pair(12);
     k.h = word(8); k.team = word(9); k.part = word(10); k.step = word(11);
-    left.flags = word(12); left.row0 = word(13); left.nodes = word(14); left.g = word(15);
     return c;
 }
 
@@ -242,7 +238,7 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
     }
     if (leader && bad) atomicOr(p.flag, 2u);
     k.head = 0; k.h = 0; k.part = 0; k.step = 0; c.beyond = 0;
-    k.wh = all;
+    k.wh = all; k.w = 0;
     all *= p.Hkv;
     const int teams_log2 = 31 - __builtin_clz(p.teams);
     const i64 w = most((all + p.teams - 1) >> teams_log2, p.wmin);
@@ -276,7 +272,7 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
                 }
                 n = count(lo);
             }
-            if (p.words || ((i64)lo * 32 * p.weight <= w && longest < 1 << 20)) {      // (beyond, a cut's place would leave 32 bits)
+            if (p.always_parts || ((i64)lo * 32 * p.weight <= w && longest < 1 << 20)) {      // (beyond, a cut's place would leave 32 bits)
                 k.part = lo;
                 k.team = team_of((n + 7) >> 3);
                 k.pos = k.team; k.end = n;
@@ -288,6 +284,7 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
     int per_xcd = p.teams >> 3;
     if (w == p.wmin) per_xcd = min(per_xcd, (((int)all + p.wmin - 1) / p.wmin + 7) >> 3);       // (all is teams * wmin at most)
     k.team = team_of(per_xcd);
+    k.w = w;
     k.pos = least(k.team * w, all);
     k.end = least(k.pos + w, all);
     return k;
@@ -311,8 +308,8 @@ __device__ __forceinline__ bool whole_piece(const ChunkParams &p, Walk &k, const
 }
 
 // The only piece of a workgroup in the form of parts: part i of n of a block's tiles, cut behind even numbers of them (a round of two waves).
-// n, i: what is cut, and which part this is.
-__device__ __forceinline__ bool only_piece(const ChunkParams &p, Walk &k, const Chunk &c, Piece &pc, Req &rq, Left &left, int &n, int &i)
+// n, i: in how many parts the block is, and which this is.
+__device__ __forceinline__ bool only_piece(const ChunkParams &p, Walk &k, const Chunk &c, Piece &pc, Req &rq, int &n, int &i)
 {
     if (k.pos >= k.end) return false;
     const int parts = c.M ? parts_of((c.L + c.M + 31) >> 5, k.part, __builtin_amdgcn_rcpf((float)k.part)) : 0;
@@ -332,16 +329,20 @@ __device__ __forceinline__ bool only_piece(const ChunkParams &p, Walk &k, const 
     pc.rq = src; pc.g = h; pc.by = b; pc.bx = 0; pc.node0 = node0; pc.nodes = nodes;
     pc.st0 = cut(i); pc.st1 = cut(i + 1);
     pc.direct = n == 1;
-    pc.through = p.words != nullptr;
-    pc.prow0 = p.words ? k.team * FEW_ROWS : (2 * k.team + (i == 0 ? 1 : 0)) * p.wr;
-    if (n > 1 && i == 0) { left.flags = BEGUN; left.row0 = rq.q0 + node0; left.nodes = nodes; left.g = h; }
-    if (n > 1 && i == n - 1) left.flags = ENDED;
     return true;
 }
 static_assert(LEAST_PART >= 4, "a part is of two tiles or more after its cuts are moved to even numbers");
 
-// The next piece; the walk moves behind it.  False: none left.  c holds the first chunk of requests.
-__device__ __forceinline__ bool next_piece(const ChunkParams &p, Walk &k, int lane, const Chunk &c, Piece &pc, Req &rq, Left &left)
+// x / w for 0 <= x, of which the quotient is below 2^16.
+__device__ __forceinline__ int shares_in(i64 x, i64 w)
+{
+    int q = __builtin_amdgcn_readfirstlane((int)((float)x * __builtin_amdgcn_rcpf((float)w)));
+    while (q * w > x) --q;
+    while ((q + 1) * w <= x) ++q;
+    return q;
+}
+// The next piece; the walk moves behind it.  False: none left.  c holds the first chunk of requests.  n, i: in how many parts the block is, and which this is.
+__device__ __forceinline__ bool next_piece(const ChunkParams &p, Walk &k, int lane, const Chunk &c, Piece &pc, Req &rq, int &n, int &i)
 {
     while (k.pos < k.end) {
         while (k.pos - k.head >= k.wh) { k.head += k.wh; ++k.h; }
@@ -391,23 +392,27 @@ __device__ __forceinline__ bool next_piece(const ChunkParams &p, Walk &k, int la
         pc.st1 = c1 == cl ? t : tile(c1);
         const bool first = c0 == 0, last = c1 == cl;
         pc.direct = first && last;
-        pc.prow0 = (2 * k.team + (first ? 1 : 0)) * p.wr;
-        if (first && !last) { left.flags |= BEGUN; left.row0 = q0 + node0; left.nodes = nodes; left.g = k.h; }
-        if (!first && last) left.flags |= ENDED;
+        if (!pc.direct) {
+            // the shares that it lies in, but for cuts that were moved to its ends (as above): the first has MARGIN of its keys or more ahead of its end, the last
+            // as many behind its beginning
+            const i64 here = k.team * k.w;
+            i = shares_in(here + k.w - ts - cm, k.w);
+            n = i + 1 + shares_in(ts + cl - cm - here, k.w);
+        }
         return true;
     }
     return false;
 }
 
-// Parts' rows, joined in the order of their keys, each relative to the row's largest reference.  16 lanes per row, R rows 16 apart per lane; row(i, r): where part i's
-// lie.  Parts come in fp16 beside their magnitude (attn_piece.h), sums are fp32.  Up to four parts are asked for at once; the reference follows from four to four.
-// THROUGH: past this XCD's caches, to which workgroups elsewhere did not write.
-template <int D, int R, bool THROUGH, typename Row, typename Store>
+// Parts' rows, joined in the order of their keys, each relative to the row's largest reference.  16 lanes per row, R rows per lane; row(i, r): where part i's
+// lie.  Parts come in fp16 beside their magnitude (attn_piece.h), sums are fp32.  Up to B parts are asked for at once; the reference follows from B to B.
+// They are read past this XCD's caches, to which workgroups elsewhere did not write.
+template <int D, int R, int B, typename Row, typename Store>
 __device__ __forceinline__ void join_parts(const ChunkParams &p, int n, int sub, Row row, Store store)
 {
     constexpr int E = D / 16;
-    const auto ml_rsrc = __builtin_amdgcn_make_buffer_rsrc(p.ML, 0, MOST_TEAMS * FEW_ROWS * 16, 0x00027000);
-    const auto part_rsrc = __builtin_amdgcn_make_buffer_rsrc(p.Opart, 0, MOST_TEAMS * FEW_ROWS * D * 2, 0x00027000);
+    const auto ml_rsrc = __builtin_amdgcn_make_buffer_rsrc(p.ML, 0, 0x7FFFFFFF, 0x00027000);
+    const auto part_rsrc = __builtin_amdgcn_make_buffer_rsrc(p.Opart, 0, 0x7FFFFFFF, 0x00027000);
     typedef _Float16 hvec __attribute__((ext_vector_type(E)));
     typedef __bf16 bvec __attribute__((ext_vector_type(E)));
     float mmax[R], den[R], acc[R][E];
@@ -417,29 +422,24 @@ __device__ __forceinline__ void join_parts(const ChunkParams &p, int n, int sub,
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[r][e] = 0.f;
     }
-    for (int i0 = 0; i0 < n; i0 += 4) {
-        hvec part[R][4];
-        float4 ml[R][4];
+    for (int i0 = 0; i0 < n; i0 += B) {
+        hvec part[R][B];
+        float4 ml[R][B];
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < B; ++b)
             if (i0 + b < n)
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    const size_t at = row(i0 + b, r);
-                    if constexpr (THROUGH) {
-                        ml[r][b] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(ml_rsrc, (int)at * 16, 0, COHERENT));
-                        if constexpr (E == 8) part[r][b] = __builtin_bit_cast(hvec, __builtin_amdgcn_raw_buffer_load_b128(part_rsrc, (int)at * D * 2 + sub * 16, 0, COHERENT));
-                        else part[r][b] = __builtin_bit_cast(hvec, __builtin_amdgcn_raw_buffer_load_b64(part_rsrc, (int)at * D * 2 + sub * 8, 0, COHERENT));
-                    } else {
-                        ml[r][b] = *reinterpret_cast<const float4 *>(p.ML + at * 4);
-                        part[r][b] = *reinterpret_cast<const hvec *>(p.Opart + at * D + sub * E);
-                    }
+                    const int at = row(i0 + b, r);
+                    ml[r][b] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(ml_rsrc, at * 16, 0, COHERENT));
+                    if constexpr (E == 8) part[r][b] = __builtin_bit_cast(hvec, __builtin_amdgcn_raw_buffer_load_b128(part_rsrc, at * D * 2 + sub * 16, 0, COHERENT));
+                    else part[r][b] = __builtin_bit_cast(hvec, __builtin_amdgcn_raw_buffer_load_b64(part_rsrc, at * D * 2 + sub * 8, 0, COHERENT));
                 }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float mn = mmax[r];
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+            for (int b = 0; b < B; ++b)
                 if (i0 + b < n) mn = fmaxf(mn, ml[r][b].x);
             const float alpha = __builtin_amdgcn_exp2f(mmax[r] - mn);
             mmax[r] = mn;
@@ -447,7 +447,7 @@ __device__ __forceinline__ void join_parts(const ChunkParams &p, int n, int sub,
 #pragma unroll
             for (int e = 0; e < E; ++e) acc[r][e] *= alpha;
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+            for (int b = 0; b < B; ++b)
                 if (i0 + b < n) {
                     const float w = __builtin_amdgcn_exp2f(ml[r][b].x - mn), wa = w * ml[r][b].z;
                     den[r] += w * ml[r][b].y;
@@ -467,12 +467,21 @@ __device__ __forceinline__ void join_parts(const ChunkParams &p, int n, int sub,
     }
 }
 
-// Few rows: the workgroup that stores the last of a block's parts merges them all (each counts itself in; the count is back at 0 then).  Nothing waits: who is not last
-// leaves.  Rows and the count go to the memory side and come from there, where all XCDs see the same (a store is acknowledged when it is there, and only then its
-// workgroup counts itself in); with fences of the device in their place every workgroup would write its XCD's L2 back and drop what it holds of others' memory.
-template <int D>
-__device__ __forceinline__ void merge_here(const ChunkParams &p, const Piece &pc, const Req &rq, int first, int n, uint32_t *said, int tid)
+// Where part i of the block that `first` begins lies: a workgroup has room for two, one that it carries on with and one that it begins.
+__device__ __forceinline__ int part_at(const ChunkParams &p, int first, int i)
 {
+    return p.always_parts ? (first + i) * p.part_rows : (2 * (first + i) + (i == 0)) * p.part_rows;
+}
+// The workgroup that stores the last of a block's parts merges them all (each counts itself in, at the block's first share; the count is back at 0 then).  Nothing waits: who is
+// not last goes on.  Rows and the count go to the memory side and come from there, where all XCDs see the same (a store is acknowledged when it is there, and only
+// then its workgroup counts itself in); with fences of the device in their place every workgroup would write its XCD's L2 back and drop what it holds of others'
+// memory.  32 single tokens, E4M3, up to 4000 keys: 25.4 us with fences, 18.8 so, 21.3 with a second launch that merges.  With more rows per block, by the second launch
+// and so: 4 prompts of up to 1999, 32 heads of 64 (nothing is cut): 24.5, 23.0; 11 chunks of up to 361 behind 830, 8 heads of 64: 16.8, 14.2; many parts of 256 rows are the
+// other way: 8 requests of 1 to 600 rows behind up to 16384: 62, 64.
+template <int D, int THREADS>
+__device__ __forceinline__ void merge_parts(const ChunkParams &p, const Piece &pc, const Req &rq, int first, int n, uint32_t *said, int tid)
+{
+    constexpr int ROWS = THREADS / 16;                  // in one go
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");    // this wavefront's rows are stored ...
     __syncthreads();                                    // ... and all the workgroup's
     if (tid == 0) {
@@ -484,12 +493,20 @@ __device__ __forceinline__ void merge_here(const ChunkParams &p, const Piece &pc
     }
     __syncthreads();
     if (!*said) return;
-    const int x = tid >> 4, node = (x * p.ginv) >> 16, sub = tid & 15;
-    if (node >= pc.nodes) return;
-    join_parts<D, 1, true>(p, n, sub, [&](int i, int) { return (size_t)(first + i) * FEW_ROWS + x; }, [&](int, const auto &o) {
-        const size_t orow = (size_t)(rq.q0 + pc.node0 + node) * p.Hq + pc.g * p.G + (x - node * p.G);
-        *reinterpret_cast<std::decay_t<decltype(o)> *>(static_cast<__bf16 *>(p.O) + orow * D + sub * (D / 16)) = o;
-    });
+    const int sub = tid & 15, rows = pc.nodes * p.G;
+    auto join = [&](auto r_, int x0) {
+        constexpr int R = decltype(r_)::value;
+        join_parts<D, R, R == 1 ? 8 : 4>(p, n, sub, [&](int i, int r) { return part_at(p, first, i) + x0 + ROWS * r; }, [&](int r, const auto &o) {
+            const int x = x0 + ROWS * r, node = (x * p.ginv) >> 16;
+            if (node >= pc.nodes) return;
+            const size_t orow = (size_t)(rq.q0 + pc.node0 + node) * p.Hq + pc.g * p.G + (x - node * p.G);
+            *reinterpret_cast<std::decay_t<decltype(o)> *>(static_cast<__bf16 *>(p.O) + orow * D + sub * (D / 16)) = o;
+        });
+    };
+    if (rows <= ROWS) {
+        if (tid >> 4 < rows) join(std::integral_constant<int, 1>{}, tid >> 4);
+    } else
+        for (int x0 = 0; x0 < rows; x0 += 4 * ROWS) join(std::integral_constant<int, 4>{}, x0 + (tid >> 4));
 }
 
 template <int D, int RW, int KW, int NT, int EB>
@@ -497,9 +514,9 @@ __global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     // (every argument in one round trip)
-    asm volatile("" ::"s"(p.Q), "s"(p.K), "s"(p.V), "s"(p.O), "s"(p.block_table), "s"(p.q_offset), "s"(p.prefix_len), "s"(p.Opart), "s"(p.ML), "s"(p.flag), "s"(p.M),
+    asm volatile("" ::"s"(p.Q), "s"(p.K), "s"(p.V), "s"(p.O), "s"(p.block_table), "s"(p.q_offset), "s"(p.prefix_len), "s"(p.Opart), "s"(p.ML), "s"(p.flag), "s"(p.M), "s"(p.part_rows), "s"(p.always_parts),
                  "s"(p.L), "s"(p.Hq), "s"(p.Hkv), "s"(p.G), "s"(p.ginv), "s"(p.max_blocks), "s"(p.num_blocks), "s"(p.total_M), "s"(p.batch), "s"(p.wmin),
-                 "s"(p.scale_log2), "s"(p.out_scale), "s"(p.left), "s"(p.nb), "s"(p.inv_nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys), "s"(p.start), "s"(p.weight), "s"(p.inv_Hkv), "s"(p.words));
+                 "s"(p.scale_log2), "s"(p.out_scale), "s"(p.nb), "s"(p.inv_nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys), "s"(p.start), "s"(p.weight), "s"(p.inv_Hkv), "s"(p.words));
     Chunk c;
     Walk k = share_out<RW == 2, RW * KW>(p, threadIdx.x & 63, blockIdx.x == 0 && threadIdx.x < 64, c, reinterpret_cast<int *>(smem));
     using CL = ChunkLds<D, RW, KW, NT, EB>;
@@ -507,12 +524,11 @@ __global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams
     static_assert(CL::PL::BYTES % 16 == 0 && RW * KW <= 8, "what is kept");
     static_assert(RW == 2 || CL::KEPT, "the turns of whole blocks");
     if (CL::KEPT && threadIdx.x < 64) keep_chunk(kept, threadIdx.x, c);     // (barriers before it is read: those of the first piece)
-    Left left = { 0, 0, 0, 0 };
     for (bool again = false;; again = true) {
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));                   // keeps what derives from it (all addresses) from being carried across pieces
         if (again) {
-            if constexpr (CL::KEPT) c = kept_chunk(kept, tid, k, left);
+            if constexpr (CL::KEPT) c = kept_chunk(kept, tid, k);
             else c = load_chunk(p, 0, tid & 63, 0);
         }
         Piece pc = {};
@@ -520,53 +536,21 @@ __global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams
         int parts = 1, part = 0;
         bool more;
         if (RW != 2 && k.step) more = whole_piece(p, k, c, pc, rq);
-        else if (k.part) more = only_piece(p, k, c, pc, rq, left, parts, part);
-        else more = next_piece(p, k, tid & 63, c, pc, rq, left);
+        else if (k.part) more = only_piece(p, k, c, pc, rq, parts, part);
+        else more = next_piece(p, k, tid & 63, c, pc, rq, parts, part);
+        if (!more) return;
+        const int first = k.team - part;
+        pc.prow0 = part_at(p, first, part);
         const bool last = k.pos >= k.end;
-        if (!more || last) {
-            if (tid == 0 && !(RW == 2 && p.words)) p.left[k.team] = left;
-            if (!more) return;
-        } else if constexpr (CL::KEPT) keep_walk(kept, tid, k, left);
+        if constexpr (CL::KEPT)
+            if (!last) keep_walk(kept, tid, k);
         attn_piece<D, RW, KW, NT, true, EB, true>(p, smem, tid, rq, pc, [] {});
-        if constexpr (RW == 2)
-            if (parts > 1 && p.words) {
-                // every wave is done with this piece's LDS
-                merge_here<D>(p, pc, rq, k.team - part, parts, reinterpret_cast<uint32_t *>(smem), tid);
-                return;
-            }
+        if (parts > 1) merge_parts<D, RW * KW * 64>(p, pc, rq, first, parts, reinterpret_cast<uint32_t *>(smem), tid);
         if (last) return;
         // every wave is done with this piece's LDS, its own fills have landed; the stores may still be on their way
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
     }
-}
-
-// The blocks that were cut: 16 lanes per row, MERGE_ROWS rows per workgroup; workgroup (k, slice) looks at the block that share k has begun.
-constexpr int MERGE_ROWS = 32;
-template <int D>
-__global__ __launch_bounds__(256) void chunk_merge(ChunkParams p)
-{
-    asm volatile("" ::"s"(p.left), "s"(p.teams), "s"(p.wr), "s"(p.G), "s"(p.ginv), "s"(p.ML), "s"(p.Opart), "s"(p.O), "s"(p.Hq), "s"(p.out_scale));
-    const int k = blockIdx.x, lane = threadIdx.x & 63, sub = threadIdx.x & 15;
-    const Left left = p.left[k];
-    const int next = p.left[min(k + 1 + lane, p.teams - 1)].flags;
-    if (!(left.flags & BEGUN) || (int)blockIdx.y * MERGE_ROWS >= left.nodes * p.G) return;
-    // the first share behind k that ends a block ends this one (those between lie within it)
-    int n = 2;
-    unsigned long long ended = __builtin_amdgcn_ballot_w64(k + 1 + lane < p.teams && (next & ENDED));
-    for (int k0 = k + 1;;) {
-        if (ended) { n = k0 - k + __builtin_ctzll(ended) + 1; break; }
-        k0 += 64;
-        if (k0 >= p.teams) return;                      // (cannot be)
-        ended = __builtin_amdgcn_ballot_w64(k0 + lane < p.teams && (p.left[min(k0 + lane, p.teams - 1)].flags & ENDED));
-    }
-    const int x0 = blockIdx.y * MERGE_ROWS + (threadIdx.x >> 4);
-    join_parts<D, MERGE_ROWS / 16, false>(p, n, sub, [&](int i, int r) { return (size_t)(2 * (k + i) + (i == 0)) * p.wr + x0 + 16 * r; }, [&](int r, const auto &o) {
-        const int x = x0 + 16 * r, node = (x * p.ginv) >> 16;
-        if (node >= left.nodes) return;
-        const size_t orow = (size_t)(left.row0 + node) * p.Hq + left.g * p.G + (x - node * p.G);
-        *reinterpret_cast<std::decay_t<decltype(o)> *>(static_cast<__bf16 *>(p.O) + orow * D + sub * (D / 16)) = o;
-    });
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
@@ -619,19 +603,17 @@ bool cuts(int M_max, int L_max) { return (L_max + M_max + 31) / 32 > SMALL; }
 // What a row block costs besides its keys, in tiles of whole blocks: finding it, its first loads, its last steps and stores.
 int start_of(int wr, int D, int eb) { return wr == 64 ? 14 : eb == 1 ? 16 : D == 64 ? 12 : 9; }
 
-// Single tokens of few requests: parts of their keys that the workgroups merge themselves, up to two parts per place on the chip where there are few, four where the requests alone
-// may fill it.
-bool merges_inside(int batch, int M_max, int G, int Hkv) { return M_max * G <= FEW_ROWS && batch <= 64 && batch * Hkv <= 512; }
-int teams_inside(int batch, int Hkv) { return batch * Hkv <= 256 ? 512 : MOST_TEAMS; }
+// Single tokens of few requests: always parts, up to two per place on the chip where there are few, four where the requests alone may fill it.
+bool few_rows(int batch, int M_max, int G, int Hkv) { return M_max * G <= FEW_ROWS && batch <= 64 && batch * Hkv <= 512; }
+int teams_of_few(int batch, int Hkv) { return batch * Hkv <= 256 ? 512 : MOST_TEAMS; }
 
-struct WsLayout { size_t left, ml, opart, total; };
+struct WsLayout { size_t ml, opart, total; };
 WsLayout ws_layout(int block_rows, int D, bool cut)
 {
     WsLayout w;
     size_t off = BTV_WS_HEADER + MERGE_WORDS;
     const size_t rows = cut ? (size_t)block_rows * 2 : 0;               // (of all workgroups; more than MOST_TEAMS * FEW_ROWS, which the parts of few rows take)
     static_assert(512 * 2 * 64 >= MOST_TEAMS * FEW_ROWS, "parts of few rows have room where shares of 64 rows have");
-    w.left = off; off += MOST_TEAMS * sizeof(Left);
     w.ml = off; off += rows * 16;
     w.opart = off; off += rows * D * 2;
     w.total = btv_align_up(off, BTV_WS_ALIGN);
@@ -693,16 +675,18 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     p.inv_Hkv = reciprocal(Hkv);
     p.max_blocks = max_blocks; p.num_blocks = num_blocks; p.total_M = total_M; p.batch = batch;
     p.scale_log2 = factor; p.out_scale = v_scale;
-    p.left = reinterpret_cast<Left *>(w8 + wl.left);
     p.wr = wr; p.nb = wr / G; p.inv_nb = reciprocal(p.nb); p.teams = sh.teams;
     p.start = start_of(wr, D, eb) * 32 * WHOLE;
     p.wmin = p.start + 8 * 32 * WHOLE;
     p.weight = (i64)M_max * G * 2 <= wr ? PART : WHOLE;
     p.most_keys = (int)std::min<i64>((i64)max_blocks * BTV_PAGE, INT_MAX);
-    const bool inside = merges_inside(batch, M_max, G, Hkv) && L_max + M_max < 1 << 25;        // (in a part's place tiles times parts stay in 32 bits)
-    if (inside) {
-        p.words = reinterpret_cast<MergeWords *>(w8 + BTV_WS_HEADER);
-        p.teams = teams_inside(batch, Hkv);
+    const bool few = few_rows(batch, M_max, G, Hkv) && L_max + M_max < 1 << 25;        // (in a part's place tiles times parts stay in 32 bits)
+    p.words = reinterpret_cast<MergeWords *>(w8 + BTV_WS_HEADER);
+    p.part_rows = wr;
+    if (few) {
+        p.always_parts = 1;
+        p.part_rows = FEW_ROWS;
+        p.teams = teams_of_few(batch, Hkv);
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define BTV_CASE(DD, EE, RR, KK, NN) if (D == DD && eb == EE && wr == RR * 32 && sh.key_waves == KK) rc = launch<DD, RR, KK, NN, EE>(p, st); else
@@ -711,12 +695,7 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     BTV_CASE(128, 1, 2, 2, 5) BTV_CASE(128, 1, 4, 2, 8)
     return btv_fail(BTV_EINVAL, "no kernel for D=%d", D);
 #undef BTV_CASE
-    if (rc || !cut || inside) return rc;
-    const dim3 grid(p.teams, wr / MERGE_ROWS);
-    if (D == 64) hipLaunchKernelGGL(chunk_merge<64>, grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL(chunk_merge<128>, grid, dim3(256), 0, st, p);
-    BTV_HIP(hipGetLastError());
-    return BTV_OK;
+    return rc;
 }
 
 }  // namespace
