@@ -417,6 +417,7 @@ int btv_kv_commit_paged(void *Kpool, void *Vpool, int layers, long long layer_st
  *                L_r + depth - 1.  slot -1 and position 0: the request did not get its pages, or the row
  *                is past the last request's; rope_append passes such rows over.
  *   n_pages_out  [batch] = P_r + t_r, n_free_out [1]; neither may be its input.
+ * No output may overlap an input or another output, block_table aside.
  * Pages stay with a request until the caller puts them back: behind the free list's last valid
  * entry, *n_free raised.  ws (optional, BTV_WS_HEADER's 256 bytes) receives the data flag: a request
  * without its pages or with lengths out of range (counted as M_r rows, or 0 if that is negative),

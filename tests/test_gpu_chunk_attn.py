@@ -335,6 +335,37 @@ def test_two_streams_with_workspaces_of_their_own():
     assert all(torch.equal(O, a) for O, a in zip(Os, alone))
 
 
+def test_two_graphs_take_turns_with_one_workspace():
+    """Calls of other shapes on one workspace, recorded apart and replayed in turn: single tokens in parts, shares with cuts, whole blocks, small row blocks."""
+    import torch
+    bs = [make(70, [5000, 30], [1, 1], 8, 2, 128, "bf16"), make(71, [3000, 0, 50], [900, 1500, 70], 8, 2, 128, "bf16"), make(72, [0] * 9, [700, 65, 300] * 3, 8, 2, 128, "bf16"),
+          make(73, [2500], [100], 8, 2, 128, "bf16")]
+    ws = max((workspace(b) for b in bs), key=lambda w: w.numel())
+    Os, graphs, side = [torch.full_like(b["Q"], 123.0) for b in bs], [torch.cuda.CUDAGraph() for _ in bs], torch.cuda.Stream()
+    alone = [run(b) for b in bs]
+    with torch.cuda.stream(side):
+        for b, O, g in zip(bs, Os, graphs):
+            with torch.cuda.graph(g, stream=side):
+                call(b, O, ws)
+    torch.cuda.synchronize()
+    for turn in ([0, 1, 2, 3], [3, 1, 0, 2], [1, 1, 3, 0], [2, 0, 2, 1]):
+        for i in turn:
+            Os[i].fill_(123.0)
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(Os[i], alone[i]) for i in turn)
+
+
+def test_the_most_requests_and_heads():
+    rng = np.random.default_rng(74)
+    b = make(74, rng.integers(0, 70, 4096).tolist(), rng.integers(0, 3, 4096).tolist(), 2, 1, 64, "bf16")
+    check(b, run(b), only=set(rng.choice(4096, 200, replace=False).tolist()) | {0, 4095})
+    b = make(75, [50, 300, 0], [3, 1, 40], 1024, 1024, 64, "bf16")
+    check(b, run(b))
+    b = make(76, [50, 300, 0], [3, 1, 40], 1024, 64, 128, "fp8")
+    check(b, run(b))
+
+
 def test_no_rows_at_all():
     import torch
     b = make(60, [40, 8], [0, 0], 8, 2, 128, "bf16")
