@@ -24,8 +24,8 @@ typedef long long i64;
 
 constexpr int WHOLE = 3, PART = 2;                              // weights of a key
 constexpr int MARGIN = 2, SMALL = 8;                            // tiles: a cut nearer to a block's ends moves there; blocks of up to SMALL are not cut
-constexpr int LEAST_PART = 4;                                   // tiles of the smallest part
-constexpr int MOST_ROWS = 1 << 20, MOST_TEAMS = 1024;
+constexpr int LEAST_PART = 8, LEAST_OF_FEW = 4, UNCUT = 16;     // tiles of the smallest part (of few rows); blocks of up to UNCUT are not worth a merge
+constexpr int MOST_ROWS = 1 << 20, MOST_TEAMS = 512;
 constexpr int FEW_ROWS = 16;                                   // of single tokens' blocks, whose parts have less room
 
 struct ChunkParams : AttnParams {
@@ -39,6 +39,7 @@ struct ChunkParams : AttnParams {
     int part_rows;                // a workgroup's room for a part's rows
     MergeWords *words;            // how many of a block's parts are stored
     int always_parts;             // few rows: parts whatever the shares would be
+    int least_part;               // tiles
 };
 
 // 64-bit minimum and maximum of numbers less than 2^62 apart, by the sign of their difference.  (Of values that a wavefront has in common the compiler makes a vector
@@ -175,7 +176,7 @@ __device__ __forceinline__ int divided(int n, int d, float inv)
     q -= r < 0;
     return q;
 }
-__device__ __forceinline__ int parts_of(int t, int part, float inv) { return divided(t + part - 1, part, inv); }
+__device__ __forceinline__ int parts_of(int t, int part, float inv) { return t <= UNCUT ? 1 : divided(t + part - 1, part, inv); }
 
 // The order of whole blocks: the longest first, of all requests, a block's KV heads beside each other.  Turn by turn the workgroups take one each, back and
 // forth, so that who had a long one has a short one next; eight neighbours stay in their order, and so on their XCD's KV heads.  Lengths count in 64 steps of
@@ -258,21 +259,25 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
         k.step = 0;
         if (all_blocks <= p.teams && all_blocks > 0) {
             // (not below what the work comes to for each, rounded down)
-            int lo = max(LEAST_PART, (int)((float)(all - (i64)all_blocks * p.start) * (0.999f / 32) / (float)(p.weight * p.teams))), n = all_blocks;
+            int lo = max(p.least_part, (int)((float)(all - (i64)all_blocks * p.start) * (0.999f / 32) / (float)(p.weight * p.teams))), n = all_blocks;
+            auto count = [&](int part) {
+                return __builtin_amdgcn_readlane(wave_sums(t ? blocks * parts_of(t, part, __builtin_amdgcn_rcpf((float)part)) : 0), 63) * p.Hkv;
+            };
             // what parts save has to be worth their merge
             if ((longest - lo) * 32 * p.weight < p.start / 4) lo = max(lo, longest);
             else {
                 int hi = longest;
-                auto count = [&](int part) {
-                    return __builtin_amdgcn_readlane(wave_sums(t ? blocks * parts_of(t, part, __builtin_amdgcn_rcpf((float)part)) : 0), 63) * p.Hkv;
-                };
                 while (lo < hi) {
                     const int mid = (lo + hi) >> 1;
                     if (count(mid) <= p.teams) hi = mid; else lo = mid + 1;
                 }
-                n = count(lo);
             }
             if (p.always_parts || ((i64)lo * 32 * p.weight <= w && longest < 1 << 20)) {      // (beyond, a cut's place would leave 32 bits)
+                // A part takes its tiles' time, and a while of the merge: the longest block is through the earliest with parts of about the root of its tiles (that
+                // ratio, measured).  With the smallest parts that there are workgroups for, of 4 tiles or more, one token over 26907 keys, 2 KV heads, took 66.5 us
+                // (now 24); 2 over 20582, E4M3, 28.5 (17.8); a chunk behind 2468 11.8 (8.4).
+                lo = max(lo, __builtin_amdgcn_readfirstlane((int)__builtin_amdgcn_sqrtf((p.always_parts ? 1.0f : 1.5f) * (float)longest)));
+                n = count(lo);
                 k.part = lo;
                 k.team = team_of((n + 7) >> 3);
                 k.pos = k.team; k.end = n;
@@ -321,7 +326,7 @@ __device__ __forceinline__ bool only_piece(const ChunkParams &p, Walk &k, const 
     i = at - b * most_parts;
     rq.q0 = __builtin_amdgcn_readlane(c.q0, src); rq.L = __builtin_amdgcn_readlane(c.L, src); rq.M = __builtin_amdgcn_readlane(c.M, src);
     const int node0 = b * p.nb, nodes = min(p.nb, rq.M - node0), t = (rq.L + node0 + nodes + 31) >> 5;
-    n = t <= SMALL ? 1 : min(most_parts, t / LEAST_PART);      // (a block of few keys: fewer parts, the other workgroups have nothing)
+    n = t <= UNCUT ? 1 : min(most_parts, t / p.least_part);      // (a block of few keys: fewer parts, the other workgroups have nothing)
     k.pos = k.end;
     if (i >= n) return false;
     const float inv = __builtin_amdgcn_rcpf((float)n);
@@ -331,7 +336,7 @@ __device__ __forceinline__ bool only_piece(const ChunkParams &p, Walk &k, const 
     pc.direct = n == 1;
     return true;
 }
-static_assert(LEAST_PART >= 4, "a part is of two tiles or more after its cuts are moved to even numbers");
+static_assert(LEAST_PART >= 4 && LEAST_OF_FEW >= 4, "a part is of two tiles or more after its cuts are moved to even numbers");
 
 // x / w for 0 <= x, of which the quotient is below 2^16.
 __device__ __forceinline__ int shares_in(i64 x, i64 w)
@@ -514,7 +519,7 @@ __global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     // (every argument in one round trip)
-    asm volatile("" ::"s"(p.Q), "s"(p.K), "s"(p.V), "s"(p.O), "s"(p.block_table), "s"(p.q_offset), "s"(p.prefix_len), "s"(p.Opart), "s"(p.ML), "s"(p.flag), "s"(p.M), "s"(p.part_rows), "s"(p.always_parts),
+    asm volatile("" ::"s"(p.Q), "s"(p.K), "s"(p.V), "s"(p.O), "s"(p.block_table), "s"(p.q_offset), "s"(p.prefix_len), "s"(p.Opart), "s"(p.ML), "s"(p.flag), "s"(p.M), "s"(p.part_rows), "s"(p.always_parts), "s"(p.least_part),
                  "s"(p.L), "s"(p.Hq), "s"(p.Hkv), "s"(p.G), "s"(p.ginv), "s"(p.max_blocks), "s"(p.num_blocks), "s"(p.total_M), "s"(p.batch), "s"(p.wmin),
                  "s"(p.scale_log2), "s"(p.out_scale), "s"(p.nb), "s"(p.inv_nb), "s"(p.wr), "s"(p.teams), "s"(p.most_keys), "s"(p.start), "s"(p.weight), "s"(p.inv_Hkv), "s"(p.words));
     Chunk c;
@@ -603,9 +608,9 @@ bool cuts(int M_max, int L_max) { return (L_max + M_max + 31) / 32 > SMALL; }
 // What a row block costs besides its keys, in tiles of whole blocks: finding it, its first loads, its last steps and stores.
 int start_of(int wr, int D, int eb) { return wr == 64 ? 14 : eb == 1 ? 16 : D == 64 ? 12 : 9; }
 
-// Single tokens of few requests: always parts, up to two per place on the chip where there are few, four where the requests alone may fill it.
-bool few_rows(int batch, int M_max, int G, int Hkv) { return M_max * G <= FEW_ROWS && batch <= 64 && batch * Hkv <= 512; }
-int teams_of_few(int batch, int Hkv) { return batch * Hkv <= 256 ? 512 : MOST_TEAMS; }
+// Single tokens of requests that have a place on the chip each: always parts.  (With up to four parts per place where the requests alone fill it: 43 requests of up to 2305 keys,
+// 8 KV heads, 23.7 us, with one 18.1; 43 of up to 5520, E4M3, 48.8 and 49.6.)
+bool few_rows(int batch, int M_max, int G, int Hkv) { return M_max * G <= FEW_ROWS && batch <= 64 && batch * Hkv <= MOST_TEAMS; }
 
 struct WsLayout { size_t ml, opart, total; };
 WsLayout ws_layout(int block_rows, int D, bool cut)
@@ -683,10 +688,10 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     const bool few = few_rows(batch, M_max, G, Hkv) && L_max + M_max < 1 << 25;        // (in a part's place tiles times parts stay in 32 bits)
     p.words = reinterpret_cast<MergeWords *>(w8 + BTV_WS_HEADER);
     p.part_rows = wr;
+    p.least_part = few ? LEAST_OF_FEW : LEAST_PART;
     if (few) {
         p.always_parts = 1;
         p.part_rows = FEW_ROWS;
-        p.teams = teams_of_few(batch, Hkv);
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
 #define BTV_CASE(DD, EE, RR, KK, NN) if (D == DD && eb == EE && wr == RR * 32 && sh.key_waves == KK) rc = launch<DD, RR, KK, NN, EE>(p, st); else
