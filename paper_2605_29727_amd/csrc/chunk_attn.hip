@@ -13,6 +13,11 @@
 // workgroup's own place in the workspace (two at most: a block that it carries on with, one that it begins), and the workgroup that stores the last of them joins them in the order of the keys.
 // Neighbouring shares are on one XCD, which so keeps to one KV head or two, whose K/V its workgroups meet in their L2.  Where there are fewer blocks than workgroups, blocks go
 // in even parts instead, and where there are more, but a few for each workgroup at most and of lengths that come out even, whole blocks in turns.
+//
+// A chunk of 2048 tokens behind 30720, 64 heads of 128 (8 of K/V): 1.83 ms, 1.16 PFLOP/s (a bf16 product of 8192^3: 1.40), behind 8192 with 32 heads 295 us, 1.05; of a tile's
+// 0.93 us the matrix instructions alone take 0.6 to 0.7 at the clock that they leave, the exponentials and the LDS reads the rest.  32 tokens over 100 to 4000 keys,
+// E4M3, 51 MB: 19 us.  Blocks of few tiles are bound by a piece's ends (us, 256 rows of 128): finding it 1.4, the first loads 2 to 3, the first scores 1.2, the last products
+// 1.1, the masked tiles 1.5, the last sums 1.4, stores 1.
 #include "attn_piece.h"
 
 #include <atomic>
