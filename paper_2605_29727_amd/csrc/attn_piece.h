@@ -925,7 +925,7 @@ struct PageLds {
 // begun(): called once the first loads are on their way (by all threads).
 // CAUSAL: rows of a chunk of a sequence in place of a tree's.  A row block then holds whole nodes (pc_.nodes from pc_.node0 on, G rows each), a row sees
 // every key up to its own, what is plain is what all rows of the block see, and the queries are not scaled.
-template <int D, int RW, int KW, int NT, bool PAGED, int EB, bool CAUSAL = false, typename Begun>
+template <int D, int RW, int KW, int NT, bool PAGED, int EB, bool CAUSAL = false, bool THROUGH = true, typename Begun>
 __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *smem, int tid, const Req &rq_, const Piece &pc_, Begun begun)
 {
     static_assert(EB == 2 || (EB == 1 && KW >= 2), "FP8 K/V runs in the shapes whose waves alternate over the tiles");
@@ -1626,7 +1626,7 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
             const h2 lo = { (_Float16)fin[dt][q * 4 + 0], (_Float16)fin[dt][q * 4 + 1] }, hi = { (_Float16)fin[dt][q * 4 + 2], (_Float16)fin[dt][q * 4 + 3] };
             return make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
         };
-        if constexpr (CAUSAL) {
+        if constexpr (CAUSAL && THROUGH) {
             // past this XCD's caches: a workgroup elsewhere may merge them (all parts lie within 2^31 bytes)
             const auto rows = __builtin_amdgcn_make_buffer_rsrc(p.Opart, 0, 0x7FFFFFFF, 0x00027000), ml = __builtin_amdgcn_make_buffer_rsrc(p.ML, 0, 0x7FFFFFFF, 0x00027000);
 #pragma unroll

@@ -10,7 +10,8 @@
 // The host knows bounds on the lengths only, so the workgroups share the work out themselves.  A row block is START + weight * keys long (the keys that its last node sees;
 // the weight is WHOLE, or PART where no more than half of the block's rows exist and a tile goes faster); blocks lie one after the other, request
 // after request, KV head after KV head, and workgroup k takes what lies between k w and (k + 1) w.  Where that cuts a block, each part's rows go to the
-// workgroup's own place in the workspace (two at most: a block that it carries on with, one that it begins), and the workgroup that stores the last of them joins them in the order of the keys.
+// workgroup's own place in the workspace (two at most: a block that it carries on with, one that it begins), and the workgroup that stores the last of them joins them in the order of the keys
+// (of 256 rows and longer work a second launch).
 // Neighbouring shares are on one XCD, which so keeps to one KV head or two, whose K/V its workgroups meet in their L2.  Where there are fewer blocks than workgroups, blocks go
 // in even parts instead, and where there are more, but a few for each workgroup at most and of lengths that come out even, whole blocks in turns.
 //
@@ -33,7 +34,11 @@ constexpr int LEAST_PART = 8, LEAST_OF_FEW = 4, UNCUT = 16;     // tiles of the 
 constexpr int MOST_ROWS = 1 << 20, MOST_TEAMS = 512;
 constexpr int FEW_ROWS = 16;                                   // of single tokens' blocks, whose parts have less room
 
+// The cut block that a workgroup begins, for the merge behind: its parts (0: none), and its first row of Q and O as [total_M].
+struct Begun { int parts, row0, nodes, g; };
+
 struct ChunkParams : AttnParams {
+    Begun *begun;                 // [teams], for a merge by a launch behind (null: by the workgroups)
     int nb;                       // nodes per row block
     uint32_t inv_nb;              // for quotient()
     int wr;                       // rows per row block
@@ -416,8 +421,8 @@ __device__ __forceinline__ bool next_piece(const ChunkParams &p, Walk &k, int la
 
 // Parts' rows, joined in the order of their keys, each relative to the row's largest reference.  16 lanes per row, R rows per lane; row(i, r): where part i's
 // lie.  Parts come in fp16 beside their magnitude (attn_piece.h), sums are fp32.  Up to B parts are asked for at once; the reference follows from B to B.
-// They are read past this XCD's caches, to which workgroups elsewhere did not write.
-template <int D, int R, int B, typename Row, typename Store>
+// THROUGH: past this XCD's caches, to which workgroups elsewhere did not write.
+template <int D, int R, int B, bool THROUGH, typename Row, typename Store>
 __device__ __forceinline__ void join_parts(const ChunkParams &p, int n, int sub, Row row, Store store)
 {
     constexpr int E = D / 16;
@@ -441,9 +446,10 @@ __device__ __forceinline__ void join_parts(const ChunkParams &p, int n, int sub,
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     const int at = row(i0 + b, r);
-                    ml[r][b] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(ml_rsrc, at * 16, 0, COHERENT));
-                    if constexpr (E == 8) part[r][b] = __builtin_bit_cast(hvec, __builtin_amdgcn_raw_buffer_load_b128(part_rsrc, at * D * 2 + sub * 16, 0, COHERENT));
-                    else part[r][b] = __builtin_bit_cast(hvec, __builtin_amdgcn_raw_buffer_load_b64(part_rsrc, at * D * 2 + sub * 8, 0, COHERENT));
+                    constexpr int SCOPE = THROUGH ? COHERENT : 0;
+                    ml[r][b] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(ml_rsrc, at * 16, 0, SCOPE));
+                    if constexpr (E == 8) part[r][b] = __builtin_bit_cast(hvec, __builtin_amdgcn_raw_buffer_load_b128(part_rsrc, at * D * 2 + sub * 16, 0, SCOPE));
+                    else part[r][b] = __builtin_bit_cast(hvec, __builtin_amdgcn_raw_buffer_load_b64(part_rsrc, at * D * 2 + sub * 8, 0, SCOPE));
                 }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
@@ -485,9 +491,10 @@ __device__ __forceinline__ int part_at(const ChunkParams &p, int first, int i)
 // The workgroup that stores the last of a block's parts merges them all (each counts itself in, at the block's first share; the count is back at 0 then).  Nothing waits: who is
 // not last goes on.  Rows and the count go to the memory side and come from there, where all XCDs see the same (a store is acknowledged when it is there, and only
 // then its workgroup counts itself in); with fences of the device in their place every workgroup would write its XCD's L2 back and drop what it holds of others'
-// memory.  32 single tokens, E4M3, up to 4000 keys: 25.4 us with fences, 18.8 so, 21.3 with a second launch that merges.  With more rows per block, by the second launch
-// and so: 4 prompts of up to 1999, 32 heads of 64 (nothing is cut): 24.5, 23.0; 11 chunks of up to 361 behind 830, 8 heads of 64: 16.8, 14.2; many parts of 256 rows are the
-// other way: 8 requests of 1 to 600 rows behind up to 16384: 62, 64.
+// memory.  32 single tokens, E4M3, up to 4000 keys: 25.4 us with fences, 18.8 so, 21.3 with a second launch that merges.  With 64 and 128 rows, by a second launch
+// and so: 4 prompts of up to 1999, 32 heads of 64 (nothing is cut): 24.5, 23.0; 11 chunks of up to 361 behind 830, 8 heads of 64: 16.8, 14.2.  With 256 one CU reads 64 KB a part: 6 prompts
+// of up to 1104, 32 heads of 64: 20.4, 18.0; 8 requests of 1 to 600 rows behind up to 16384: 62.3, 64.3; a chunk of 2048 behind 8192: 286.8, 290.8 (one by one 334, 351).  There the launch
+// stays where each workgroup has more than 30 tiles' work.
 template <int D, int THREADS>
 __device__ __forceinline__ void merge_parts(const ChunkParams &p, const Piece &pc, const Req &rq, int first, int n, uint32_t *said, int tid)
 {
@@ -506,7 +513,7 @@ __device__ __forceinline__ void merge_parts(const ChunkParams &p, const Piece &p
     const int sub = tid & 15, rows = pc.nodes * p.G;
     auto join = [&](auto r_, int x0) {
         constexpr int R = decltype(r_)::value;
-        join_parts<D, R, R == 1 ? 8 : 4>(p, n, sub, [&](int i, int r) { return part_at(p, first, i) + x0 + ROWS * r; }, [&](int r, const auto &o) {
+        join_parts<D, R, R == 1 ? 8 : 4, true>(p, n, sub, [&](int i, int r) { return part_at(p, first, i) + x0 + ROWS * r; }, [&](int r, const auto &o) {
             const int x = x0 + ROWS * r, node = (x * p.ginv) >> 16;
             if (node >= pc.nodes) return;
             const size_t orow = (size_t)(rq.q0 + pc.node0 + node) * p.Hq + pc.g * p.G + (x - node * p.G);
@@ -519,7 +526,7 @@ __device__ __forceinline__ void merge_parts(const ChunkParams &p, const Piece &p
         for (int x0 = 0; x0 < rows; x0 += 4 * ROWS) join(std::integral_constant<int, 4>{}, x0 + (tid >> 4));
 }
 
-template <int D, int RW, int KW, int NT, int EB>
+template <int D, int RW, int KW, int NT, int EB, bool BEHIND>
 __global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams p)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -548,19 +555,41 @@ __global__ __launch_bounds__(RW * KW * 64, 2) void chunk_attn_kernel(ChunkParams
         if (RW != 2 && k.step) more = whole_piece(p, k, c, pc, rq);
         else if (k.part) more = only_piece(p, k, c, pc, rq, parts, part);
         else more = next_piece(p, k, tid & 63, c, pc, rq, parts, part);
-        if (!more) return;
+        if (!more) {
+            if (BEHIND && tid == 0) p.begun[k.team] = Begun{ 0, 0, 0, 0 };
+            return;
+        }
         const int first = k.team - part;
         pc.prow0 = part_at(p, first, part);
         const bool last = k.pos >= k.end;
+        // (a workgroup begins one cut block at most, with its last piece)
+        if (BEHIND && last && tid == 0) p.begun[k.team] = parts > 1 && part == 0 ? Begun{ parts, rq.q0 + pc.node0, pc.nodes, pc.g } : Begun{ 0, 0, 0, 0 };
         if constexpr (CL::KEPT)
             if (!last) keep_walk(kept, tid, k);
-        attn_piece<D, RW, KW, NT, true, EB, true>(p, smem, tid, rq, pc, [] {});
-        if (parts > 1) merge_parts<D, RW * KW * 64>(p, pc, rq, first, parts, reinterpret_cast<uint32_t *>(smem), tid);
+        attn_piece<D, RW, KW, NT, true, EB, true, !BEHIND>(p, smem, tid, rq, pc, [] {});
+        if (!BEHIND && parts > 1) merge_parts<D, RW * KW * 64>(p, pc, rq, first, parts, reinterpret_cast<uint32_t *>(smem), tid);
         if (last) return;
         // every wave is done with this piece's LDS, its own fills have landed; the stores may still be on their way
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
     }
+}
+
+// The blocks of 256 rows that were cut: 16 lanes per row, MERGE_ROWS rows per workgroup; workgroup (k, slice) looks at the block that workgroup k has begun.
+constexpr int MERGE_ROWS = 32;
+template <int D>
+__global__ __launch_bounds__(256) void chunk_merge(ChunkParams p)
+{
+    asm volatile("" ::"s"(p.begun), "s"(p.part_rows), "s"(p.always_parts), "s"(p.G), "s"(p.ginv), "s"(p.ML), "s"(p.Opart), "s"(p.O), "s"(p.Hq), "s"(p.out_scale));
+    const int k = blockIdx.x, sub = threadIdx.x & 15, x0 = blockIdx.y * MERGE_ROWS + (threadIdx.x >> 4);
+    const Begun b = p.begun[k];
+    if (b.parts == 0 || (int)blockIdx.y * MERGE_ROWS >= b.nodes * p.G) return;
+    join_parts<D, MERGE_ROWS / 16, 4, false>(p, b.parts, sub, [&](int i, int r) { return part_at(p, k, i) + x0 + 16 * r; }, [&](int r, const auto &o) {
+        const int x = x0 + 16 * r, node = (x * p.ginv) >> 16;
+        if (node >= b.nodes) return;
+        const size_t orow = (size_t)(b.row0 + node) * p.Hq + b.g * p.G + (x - node * p.G);
+        *reinterpret_cast<std::decay_t<decltype(o)> *>(static_cast<__bf16 *>(p.O) + orow * D + sub * (D / 16)) = o;
+    });
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
@@ -593,20 +622,20 @@ int most_rows(int M_max, int G, int eb)
 // With 64 channels two workgroups of 128 rows, four waves that take every tile, fit on a CU: of many blocks one's ends pass while the other computes, but each brings its own
 // tiles.  us with 256 rows and so: 6 prompts of up to 2348, 16 heads: 41.7, 34.9 (396 blocks, 57 tiles); 26 of up to 125, 32 heads: 17.6, 9.0 (258, 2); 34 chunks of up to
 // 545 behind 4275, 16 heads: 65.2, 65.6 (454, 252); 7 of up to 551 behind 25259, 16 heads: 70.2, 76.8 (141, 440).
-struct Shape { int rows, key_waves, teams; };
+struct Shape { int rows, key_waves, teams; bool behind; };      // behind: merged by a launch
 Shape shape_of(int batch, int total_M, int M_max, int L_max, int G, int Hkv, int D, int eb)
 {
     const int most = most_rows(M_max, G, eb);
     const double rows = (double)total_M * G, half = 0.5 * batch;
     const double tiles = (rows / 256 + half) * Hkv * ((double)L_max + 0.5 * M_max) / (32 * 256);
-    if ((rows / 64 + half) * Hkv <= 512 && tiles <= 30) return { 64, 2, 512 };
-    if (most <= 64) return { 64, 2, 512 };
+    if ((rows / 64 + half) * Hkv <= 512 && tiles <= 30) return { 64, 2, 512, false };
+    if (most <= 64) return { 64, 2, 512, false };
     // (very short ones: a second turn costs as much as the first; 37 prompts of up to 234, 16 heads of 128: 15.4 with 256 rows, 22.9 with 128; 8 of up to 479, 32 heads, where
     // 7 tiles come to each: 26.2, 22.3)
     const bool few = (rows / 256 + half) * Hkv <= 256 && (tiles >= 4 || (rows / 128 + half) * Hkv <= 256);
-    if (most == 128 || (few && tiles <= 110)) return { 128, 2, 256 };
-    if (D == 64 && !few && tiles <= 200) return { 128, 1, 512 };
-    return { 256, 1, 256 };
+    if (most == 128 || (few && tiles <= 110)) return { 128, 2, 256, false };
+    if (D == 64 && !few && tiles <= 200) return { 128, 1, 512, false };
+    return { 256, 1, 256, tiles > 30 };
 }
 bool cuts(int M_max, int L_max) { return (L_max + M_max + 31) / 32 > SMALL; }
 
@@ -617,13 +646,14 @@ int start_of(int wr, int D, int eb) { return wr == 64 ? 14 : eb == 1 ? 16 : D ==
 // 8 KV heads, 23.7 us, with one 18.1; 43 of up to 5520, E4M3, 48.8 and 49.6.)
 bool few_rows(int batch, int M_max, int G, int Hkv) { return M_max * G <= FEW_ROWS && batch <= 64 && batch * Hkv <= MOST_TEAMS; }
 
-struct WsLayout { size_t ml, opart, total; };
+struct WsLayout { size_t begun, ml, opart, total; };
 WsLayout ws_layout(int block_rows, int D, bool cut)
 {
     WsLayout w;
     size_t off = BTV_WS_HEADER + MERGE_WORDS;
     const size_t rows = cut ? (size_t)block_rows * 2 : 0;               // (of all workgroups; more than MOST_TEAMS * FEW_ROWS, which the parts of few rows take)
     static_assert(512 * 2 * 64 >= MOST_TEAMS * FEW_ROWS, "parts of few rows have room where shares of 64 rows have");
+    w.begun = off; off += MOST_TEAMS * sizeof(Begun);
     w.ml = off; off += rows * 16;
     w.opart = off; off += rows * D * 2;
     w.total = btv_align_up(off, BTV_WS_ALIGN);
@@ -634,7 +664,7 @@ size_t enough_for(int M_max, int L_max, int G, int D, int eb)
     return ws_layout(most_rows(M_max, G, eb) > 128 ? 256 * 256 : 256 * 128, D, cuts(M_max, L_max)).total;
 }
 
-template <int D, int RW, int KW, int NT, int EB>
+template <int D, int RW, int KW, int NT, int EB, bool BEHIND>
 int launch(const ChunkParams &p, hipStream_t st)
 {
     constexpr int LDS_BYTES = ChunkLds<D, RW, KW, NT, EB>::BYTES;
@@ -644,10 +674,10 @@ int launch(const ChunkParams &p, hipStream_t st)
     BTV_HIP(hipGetDevice(&dev));
     const unsigned long long bit = 1ull << (dev & 63);
     if (!(configured.load(std::memory_order_acquire) & bit)) {
-        BTV_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(chunk_attn_kernel<D, RW, KW, NT, EB>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES));
+        BTV_HIP(hipFuncSetAttribute(reinterpret_cast<const void *>(chunk_attn_kernel<D, RW, KW, NT, EB, BEHIND>), hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES));
         configured.fetch_or(bit, std::memory_order_release);
     }
-    hipLaunchKernelGGL((chunk_attn_kernel<D, RW, KW, NT, EB>), dim3(p.teams), dim3(RW * KW * 64), LDS_BYTES, st, p);
+    hipLaunchKernelGGL((chunk_attn_kernel<D, RW, KW, NT, EB, BEHIND>), dim3(p.teams), dim3(RW * KW * 64), LDS_BYTES, st, p);
     BTV_HIP(hipGetLastError());
     return BTV_OK;
 }
@@ -692,6 +722,8 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     p.most_keys = (int)std::min<i64>((i64)max_blocks * BTV_PAGE, INT_MAX);
     const bool few = few_rows(batch, M_max, G, Hkv) && L_max + M_max < 1 << 25;        // (in a part's place tiles times parts stay in 32 bits)
     p.words = reinterpret_cast<MergeWords *>(w8 + BTV_WS_HEADER);
+    const bool behind = sh.behind && cut;
+    p.begun = behind ? reinterpret_cast<Begun *>(w8 + wl.begun) : nullptr;
     p.part_rows = wr;
     p.least_part = few ? LEAST_OF_FEW : LEAST_PART;
     if (few) {
@@ -699,13 +731,18 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
         p.part_rows = FEW_ROWS;
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
-#define BTV_CASE(DD, EE, RR, KK, NN) if (D == DD && eb == EE && wr == RR * 32 && sh.key_waves == KK) rc = launch<DD, RR, KK, NN, EE>(p, st); else
-    BTV_CASE(128, 2, 2, 2, 5) BTV_CASE(128, 2, 4, 2, 8) BTV_CASE(128, 2, 8, 1, 8)
-    BTV_CASE(64, 2, 2, 2, 5) BTV_CASE(64, 2, 4, 2, 8) BTV_CASE(64, 2, 4, 1, 8) BTV_CASE(64, 2, 8, 1, 8)
-    BTV_CASE(128, 1, 2, 2, 5) BTV_CASE(128, 1, 4, 2, 8)
+#define BTV_CASE(DD, EE, RR, KK, NN, BB) if (D == DD && eb == EE && wr == RR * 32 && sh.key_waves == KK && behind == BB) rc = launch<DD, RR, KK, NN, EE, BB>(p, st); else
+    BTV_CASE(128, 2, 2, 2, 5, false) BTV_CASE(128, 2, 4, 2, 8, false) BTV_CASE(128, 2, 8, 1, 8, false) BTV_CASE(128, 2, 8, 1, 8, true)
+    BTV_CASE(64, 2, 2, 2, 5, false) BTV_CASE(64, 2, 4, 2, 8, false) BTV_CASE(64, 2, 4, 1, 8, false) BTV_CASE(64, 2, 8, 1, 8, false) BTV_CASE(64, 2, 8, 1, 8, true)
+    BTV_CASE(128, 1, 2, 2, 5, false) BTV_CASE(128, 1, 4, 2, 8, false)
     return btv_fail(BTV_EINVAL, "no kernel for D=%d", D);
 #undef BTV_CASE
-    return rc;
+    if (rc || !behind) return rc;
+    const dim3 grid(p.teams, wr / MERGE_ROWS);
+    if (D == 64) hipLaunchKernelGGL(chunk_merge<64>, grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL(chunk_merge<128>, grid, dim3(256), 0, st, p);
+    BTV_HIP(hipGetLastError());
+    return BTV_OK;
 }
 
 }  // namespace

@@ -127,7 +127,7 @@ def test_work_for_all_workgroups(kv, Hq, Hkv, D, Ls, Ms):
 @pytest.mark.parametrize("kv,Hq,Hkv,D", [("bf16", 16, 8, 128), ("bf16", 32, 8, 64), ("fp8", 8, 8, 128), ("bf16", 24, 6, 128), ("bf16", 12, 12, 64), ("fp8", 7, 7, 128)])
 @pytest.mark.parametrize("Ls,Ms", [([0], [4300]), ([3000], [4096]), ([0, 0, 0, 0], [1600, 2000, 1, 1111]), ([5, 900, 0, 0, 77, 3, 40, 2000], [1800, 0, 700, 129, 1000, 65, 1500, 333]),
                                    ([20000, 0], [700, 3500]),
-                                   ([0, 9, 64] * 20, [400, 33, 170] * 20), ([0] * 30, [128, 1, 97] * 10)], ids=lambda x: "-".join(map(str, x[:8])))
+                                   ([0, 9, 64] * 20, [400, 33, 170] * 20), ([0] * 30, [128, 1, 97] * 10), ([0] * 70, [5 * i + 3 for i in range(70)])], ids=lambda x: "-".join(map(str, x[:8])))
 def test_more_blocks_than_workgroups(kv, Hq, Hkv, D, Ls, Ms):
     b = make(3 * sum(Ls) + sum(Ms), Ls, Ms, Hq, Hkv, D, kv)
     check(b, run(b))
