@@ -602,7 +602,7 @@ int check_chunk(int batch, int M_max, int L_max, int Hq, int Hkv, int D)
     BTV_REQUIRE(Hq >= 1 && Hkv >= 1 && Hkv <= 1024 && Hq % Hkv == 0 && Hq / Hkv <= 16, "bad heads Hq=%d Hkv=%d", Hq, Hkv);
     BTV_REQUIRE(D == 64 || D == 128, "D=%d not in {64,128}", D);
     // the work's length stays below 2^62, and 64 requests' of one head below 2^54 (a request and head has at most M / 4 + 1 blocks)
-    const double head = (M_max / 4 + 1) * (4096.0 + (double)WHOLE * ((double)L_max + M_max));
+    const double head = (M_max / 4 + 1) * (8192.0 + (double)WHOLE * ((double)L_max + M_max));
     BTV_REQUIRE(64 * head < 1.8e16 && batch * head * Hkv < 4.6e18, "more work than can be counted");
     return BTV_OK;
 }
@@ -639,8 +639,12 @@ Shape shape_of(int batch, int total_M, int M_max, int L_max, int G, int Hkv, int
 }
 bool cuts(int M_max, int L_max) { return (L_max + M_max + 31) / 32 > SMALL; }
 
-// What a row block costs besides its keys, in tiles of whole blocks: finding it, its first loads, its last steps and stores.
-int start_of(int wr, int D, int eb) { return wr == 64 ? 14 : eb == 1 ? 16 : D == 64 ? 12 : 9; }
+// What a row block costs besides its keys, in tiles of whole blocks: finding it, its first loads, its last steps and stores.  Parts, shares and whole blocks are weighed with
+// it.  The stamps say 8 to 12 tiles; that much and half or twice it are within 2 % on average of 120 calls.  With 128 rows 16 is the best (3 chunks of up to 232 behind 4322, 64 heads: 35.8 us
+// with 9, so 31.4; E4M3 with 22: 27 of up to 914 behind 623, 91.7, so 77.1).  64 rows are taken where all blocks find a workgroup: a large number keeps them in parts, and in
+// one piece where parts would be hardly smaller (29 chunks of up to 96 behind 1313, 28 heads: 30.5 with 14, so 24.7; 3 prompts of up to 3064: 21.9, 17.2); single
+// tokens split at less (16 over up to 1094 keys, E4M3: 16.3 with 100, with 14 12.0).
+int start_of(int wr, int D, bool few) { return few ? 14 : wr == 64 ? 60 : wr == 128 ? 16 : D == 64 ? 12 : 9; }
 
 // Single tokens of requests that have a place on the chip each: always parts.  (With up to four parts per place where the requests alone fill it: 43 requests of up to 2305 keys,
 // 8 KV heads, 23.7 us, with one 18.1; 43 of up to 5520, E4M3, 48.8 and 49.6.)
@@ -716,14 +720,14 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     p.max_blocks = max_blocks; p.num_blocks = num_blocks; p.total_M = total_M; p.batch = batch;
     p.scale_log2 = factor; p.out_scale = v_scale;
     p.wr = wr; p.nb = wr / G; p.inv_nb = reciprocal(p.nb); p.teams = sh.teams;
-    p.start = start_of(wr, D, eb) * 32 * WHOLE;
-    p.wmin = p.start + 8 * 32 * WHOLE;
     p.weight = (i64)M_max * G * 2 <= wr ? PART : WHOLE;
     p.most_keys = (int)std::min<i64>((i64)max_blocks * BTV_PAGE, INT_MAX);
     const bool few = few_rows(batch, M_max, G, Hkv) && L_max + M_max < 1 << 25;        // (in a part's place tiles times parts stay in 32 bits)
     p.words = reinterpret_cast<MergeWords *>(w8 + BTV_WS_HEADER);
     const bool behind = sh.behind && cut;
     p.begun = behind ? reinterpret_cast<Begun *>(w8 + wl.begun) : nullptr;
+    p.start = start_of(wr, D, few) * 32 * WHOLE;
+    p.wmin = p.start + 8 * 32 * WHOLE;
     p.part_rows = wr;
     p.least_part = few ? LEAST_OF_FEW : LEAST_PART;
     if (few) {
