@@ -23,8 +23,8 @@ struct ExtendParams {
     int batch, total_max, num_blocks, max_blocks, rows_per_wg;
 };
 
-// What is kept of a request in LDS for the rows: where its rows begin, its length and pages, and how many pages were taken before it (-1 where it does not get
-// what it needs).
+// What is kept of a request in LDS for the rows: where its rows begin (2^31 - 1 at most), its length and pages, and how many pages the requests before it ask for, up to
+// what the list has (x; ~x, which is negative, where it does not get what it needs).
 struct Kept { int32_t *first, *L, *P, *taken; };
 
 // Inclusive sums over the lanes (numbers below 2^54 in three pieces).
@@ -78,7 +78,8 @@ __global__ __launch_bounds__(THREADS) void paged_extend_kernel(ExtendParams p)
             const bool granted = ok && (take == 0 || page + take <= n_free);
             const int first = row < INT_MAX ? (int)row : INT_MAX;
             kept.first[r] = first; kept.L[r] = L; kept.P[r] = P;
-            kept.taken[r] = granted ? (page < n_free ? (int)page : n_free) : -1;
+            const int before = page < n_free ? (int)page : n_free;
+            kept.taken[r] = granted ? before : ~before;
             if (granted) taken_all += take;
             bad = bad || !granted || row + M > p.total_max;
             if (blockIdx.x == 0) {
@@ -123,11 +124,12 @@ __global__ __launch_bounds__(THREADS) void paged_extend_kernel(ExtendParams p)
     const long long b0 = (long long)blockIdx.x * p.rows_per_wg, b1 = min(b0 + p.rows_per_wg, (long long)p.total_max);
     for (long long x = b0 + tid; x < b1; x += THREADS) row(x);
 
-    // The table's new entries: a wavefront per request (M again from where the next one's rows begin).
+    // The table's new entries: a wavefront per request.  It takes what lies between its pages and the next one's (rows say nothing here: a request before it may be out of range, and
+    // count as more rows than there are numbers).
     for (int r = blockIdx.x * WAVES + wave; r < p.batch; r += gridDim.x * WAVES) {
-        const int base = kept.taken[r], L = kept.L[r], P = kept.P[r];
+        const int base = kept.taken[r], P = kept.P[r];
         if (base < 0) continue;
-        const int M = (r + 1 < p.batch ? kept.first[r + 1] : total) - kept.first[r], take = (L + M + (BTV_PAGE - 1)) / BTV_PAGE - P;
+        const int next = r + 1 < p.batch ? kept.taken[r + 1] : pages < n_free ? (int)pages : n_free, take = (next < 0 ? ~next : next) - base;
         for (int k = lane; k < take; k += 64) {
             const int id = p.free_pages[n_free - 1 - base - k];
             bad = bad || id < 0 || id >= p.num_blocks;

@@ -332,3 +332,17 @@ def test_on_another_stream_and_in_a_graph():
         load(i)
         step()
         assert all(torch.equal(a, b) for a, b in zip(got, shown())), i
+
+
+@pytest.mark.parametrize("batch", [2, 5, 300])
+@pytest.mark.parametrize("new", [2**31 - 1, 2**30 + 7])
+def test_extend_pages_of_requests_behind_a_length_out_of_range(batch, new):
+    """The rows of a request out of range count, so that later requests' rows begin past 2^31 - 1; they get their pages all the same."""
+    Ls = synth.integers(batch, "L", (batch,), 0, 300).tolist()
+    Ms = synth.integers(batch, "M", (batch,), 17, 130).tolist()
+    for far in ([0], [0, batch // 2], [batch - 1]):
+        c = extend_case(batch, Ls, Ms)
+        c["n_new"][far] = new
+        ref = check_extend(c, total_max=60)
+        taken = (ref["table"] != c["table"]).any(1)
+        assert ref["bad"] and not taken[far].any() and taken[[r for r in range(batch) if ref["n_pages"][r] > c["n_pages"][r]]].all()
