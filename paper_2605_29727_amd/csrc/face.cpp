@@ -475,7 +475,8 @@ PyObject *append(PyObject *const *args, Py_ssize_t n, bool fp8)
             require(fp8 ? t->element_size() == 1 && q.scalar_type() == at::kBFloat16 : t->scalar_type() == q.scalar_type(),
                     fp8 ? "one-byte caches and bfloat16 rows" : "the caches must have the rows' type");
         }
-        const long long num_slots = kc.numel() / ((long long)Hkv * D);
+        long long num_slots = 1;                        // (without a division by heads and channels, of which there may be none)
+        for (int64_t i = 0; i + 2 < kc.dim(); ++i) num_slots *= kc.size(i);
         const int32_t *position = ints(po, total), *slot = ints(sl, total);
         const double *inv_freq = typed<double>(fr, at::kDouble, "inv_freq must be a contiguous float64 CUDA tensor");
         void *out = typed(qo, q.scalar_type(), "Qout must be contiguous and of Q's type");

@@ -346,3 +346,17 @@ def test_extend_pages_of_requests_behind_a_length_out_of_range(batch, new):
         ref = check_extend(c, total_max=60)
         taken = (ref["table"] != c["table"]).any(1)
         assert ref["bad"] and not taken[far].any() and taken[[r for r in range(batch) if ref["n_pages"][r] > c["n_pages"][r]]].all()
+
+
+@pytest.mark.parametrize("Hkv,D", [(0, 128), (1, 0), (0, 0), (2, 0)])
+@pytest.mark.parametrize("T", [3, 0])
+def test_rope_append_refuses_caches_without_heads_or_channels(T, Hkv, D):
+    import torch
+    from paper_2605_29727_amd import binding as btv
+    i = torch.zeros(T, dtype=torch.int32, device="cuda")
+    f = torch.ones(8, dtype=torch.float64, device="cuda")
+    for dt, append, more in ((torch.bfloat16, btv.btv_rope_append, ()), (torch.uint8, btv.btv_rope_append_fp8kv, (1.0, 1.0))):
+        q, kv = torch.zeros((T, 1, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((T, Hkv, D), dtype=torch.bfloat16, device="cuda")
+        cache = torch.zeros((2, PAGE, Hkv, D), dtype=dt, device="cuda")
+        with pytest.raises((btv.BtvError, AssertionError)):       # (the library's refusal, or that such heads do not lie side by side)
+            append(q, kv, kv, i, i, f, torch.zeros_like(q), cache, cache.clone(), *more)
