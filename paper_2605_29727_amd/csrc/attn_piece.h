@@ -1137,6 +1137,16 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
 #pragma unroll
         for (int v = 0; v < 16; ++v) oacc[dt][v] = 0.f;
 
+    // A row whose first tile has no score above -infinity has no reference for the tiles behind it, which do not look for one.  It starts from -NO_SCORE: far below any
+    // maximum, so that its first finite score makes the tile's sum overflow and the tile be done again, and near enough to leave that tile's scores 2^-10.
+    // settle(): a row that has met none by the end has none, and whatever it is merged with is above it.
+    constexpr float NO_SCORE = 16384.0f;
+    auto settle = [&]() {
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(m_run == -NO_SCORE) != 0ull, 0)) {       // (rare; a maximum of just that has a sum)
+            const float sum = l_run + __shfl_xor(l_run, 32);
+            if (m_run == -NO_SCORE && sum == 0.f) m_run = NEG_BIG;
+        }
+    };
     bf16x8 qreg[DS];
     if constexpr (DS == 8)
         asm volatile("s_waitcnt lgkmcnt(0)"
@@ -1287,7 +1297,7 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
                 read_k_half_at<D, 1>(kbase, kh); wait_k_half<KH, 0>(kh); x = qk_half<DS, 1>(kh, qreg, x);
                 read_k_half_at<D, 0>(kbase + slot_off(1), kh);
                 negm = -tile_max(x);
-                if constexpr (CAUSAL) negm = negm <= FLT_MAX ? negm : 0.f;        // (a row of which this tile's scores all are -infinity)
+                negm = negm <= FLT_MAX ? negm : NO_SCORE;
 #pragma unroll
                 for (int v = 0; v < 16; ++v) x[v] += negm;
                 exp_half(x, 0, pa[0], l_run, cf);                // x <= 0 here: no growth check
@@ -1403,6 +1413,7 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
                 wait_v_half<DT, 0>(vh);
                 pv_half<DT>(vh, pn[1], oacc);
                 m_run = -negm;
+                settle();
             };
             // One iteration per trip, the new probabilities copied into place at its end (8 moves): with the roles of
             // two register sets alternating over an unrolled pair the allocator shuffles tuples and spills.
@@ -1434,10 +1445,10 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
             j0 = Tf;
         }
         // ---- the remaining tiles (those that touch tree rows, or all of a short split), step by step ----
-        if (j0 > 0) {                                            // (m_run is a real maximum after the pipelined part)
-            base = m_run;
+        if (j0 > 0) {                                            // (m_run is a maximum after the pipelined part, if there was a finite score)
+            base = m_run > 0.5f * NEG_BIG ? m_run : 0.f;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) negb[v] = -m_run;
+            for (int v = 0; v < 16; ++v) negb[v] = -base;
         }
         read_mask();                                             // (barriers since the sets were written: those of the prologue)
         for (int j = j0; j < st1 - st0; ++j) {
@@ -1474,7 +1485,15 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
         };
         // Rounds that ask for KW tiles of the prefix with all their keys, and so only take such, have nothing to test for.
         const int plain = min(st1, Lr / 32);
-        if (live && st + kwu < st1) tile(std::false_type{});     // (on its own: nothing has to be cleared ahead of it)
+        if (live && st + kwu < st1) {                            // (on its own: nothing has to be cleared ahead of it)
+            tile(std::false_type{});
+            if (__builtin_expect((st + kwu) * 32 + 32 <= Lr && __builtin_amdgcn_ballot_w64(m_run < 0.5f * NEG_BIG) != 0ull, 0)) {       // (rare)
+                const bool none = m_run < 0.5f * NEG_BIG;
+                if (none) m_run = base = -NO_SCORE;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) negb[v] = none ? NO_SCORE : negb[v];
+            }
+        }
         next_round();
         whole_tiles();
         for (; issued + KW <= plain; next_round()) {
@@ -1493,6 +1512,7 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
             begin_round(st);
             if (live && st + kwu < st1) tile(std::false_type{});
         }
+        settle();
     }
     if constexpr (CAUSAL) m_run = times(m_run, cf);
     LaneRow lrow;

@@ -480,3 +480,19 @@ def test_paged_non_finite_values_stay_in_their_channel(G):
             x[:, :8, 7] = 0
         assert (run[0] - run[1]).abs().max() <= 2.0 ** -8       # (two bf16 roundings of values below 2, partials scaled otherwise)
         assert run[0].abs().max() > 0.1
+
+
+@pytest.mark.parametrize("tiles", [[0], [1], [0, 1], [0, 1, 2, 3, 5, 8], list(range(2, 46))], ids=lambda x: f"{x[0]}..{x[-1]}x{len(x)}")
+@pytest.mark.parametrize("M,Hq,Hkv,D", [(1, 8, 2, 128), (16, 8, 2, 128), (30, 8, 2, 128), (60, 16, 2, 128), (200, 8, 2, 128), (16, 8, 2, 64), (100, 16, 4, 64)])
+def test_bf16_prefix_tiles_without_a_finite_score(G, oracle, M, Hq, Hkv, D, tiles):
+    """32 keys on end whose scores all are -infinity weigh nothing, wherever they lie and however the call is cut."""
+    L = 1500
+    parent = synth.tree_parents(5, M, "random")
+    t = synth.qkv(44, M, L, Hq, Hkv, D, "bf16")
+    keys = [32 * k + j for k in tiles for j in range(32)]
+    t["Q"][:, :, 33], t["Qf"][:, :, 33] = 0xBF80, -1.0
+    t["K"][keys, :, 33], t["Kf"][keys, :, 33] = 0x7F80, np.inf
+    ref = oracle.tree_attn(t["Qf"], t["Kf"], t["Vf"], parent, L)
+    assert np.isfinite(ref).all()
+    for nsplit in (0, 1, 3, 47):
+        assert np.abs(G.run_verify_attn(t, parent, L, "bf16", nsplit=nsplit) - ref).max() <= TOL_BF16, nsplit

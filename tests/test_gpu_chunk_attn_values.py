@@ -1,0 +1,57 @@
+"""Chunk attention (btv_chunk_attn_paged, btv_chunk_attn_paged_fp8kv) with keys, values and scales at the ends of their types."""
+import math
+
+import pytest
+
+from test_gpu_chunk_attn import PAGE, make, run
+
+pytestmark = pytest.mark.gpu
+
+
+def put(b, name, r, keys, channel, value):
+    """Sets a channel of the keys (or values) of request r, all heads."""
+    import torch
+    at = torch.as_tensor(keys, device="cuda")
+    b[name][b["table"][r].long()[at // PAGE], at % PAGE, :, channel] = value
+
+
+# Tiles of 32 keys whose scores all are -infinity: the first of a sequence, of a wavefront, of a part or anywhere, and all but a few.  low: what the other scores
+# come to besides (-3200 before the scale: a reference of 0 would leave nothing of their exponentials).
+@pytest.mark.parametrize("low", [0.0, -400.0])
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (8, 2, 64), (32, 8, 128), (4, 4, 64)])
+@pytest.mark.parametrize("L,M,tiles", [(300, 1, [0]), (300, 1, [1]), (300, 1, [0, 1]), (300, 1, [0, 1, 2, 3, 4]), (300, 40, [0]), (300, 40, [1, 2, 3]), (3000, 1, "some"), (3000, 1, "most"),
+                                       (9000, 17, "some"), (700, 100, [0, 1, 2]), (2500, 300, "some"), (2500, 300, "most"), (0, 700, [1, 2]), (0, 700, [0, 1]), (4099, 2047, "some"),
+                                       (4099, 2047, "most"), (0, 2048, [0, 2, 3])], ids=lambda x: str(x).replace(" ", ""))
+def test_infinite_keys(Hq, Hkv, D, L, M, tiles, low):
+    import torch
+    b = make(L + M + D, [L], [M], Hq, Hkv, D, "bf16")
+    n = (L + M) // 32
+    if isinstance(tiles, str):
+        g = torch.Generator().manual_seed(n)
+        tiles = torch.nonzero(torch.rand(n, generator=g) < (0.4 if tiles == "some" else 0.95)).flatten().tolist()
+    keys = [32 * t + j for t in tiles for j in range(32)]
+    assert keys[-1] < L + M
+    b["Q"][..., 33], b["Q"][..., 34] = -1.0, 8.0
+    everything = list(range(L + M))
+    put(b, "K", 0, everything, 34, low)
+    k, v = (x.double() for x in b["rows"][0])
+    k[:, :, 34] = low
+    put(b, "K", 0, keys, 33, math.inf)
+    gone = torch.zeros(L + M, dtype=torch.bool, device="cuda")
+    gone[keys] = True
+    O = run(b).double()
+    G = Hq // Hkv
+    for h in range(Hq):
+        q, kh, vh = b["Q"][:, h].double(), k[:, h // G], v[:, h // G]
+        hidden = gone | (torch.arange(L + M, device="cuda") > L + torch.arange(M, device="cuda")[:, None])
+        none = hidden.all(1)
+        w = torch.softmax((q @ kh.T * D ** -0.5).masked_fill(hidden, -math.inf), -1)
+        ref, mass = w @ vh, w @ vh.abs()
+        # Probabilities in bf16 in numerator and sum, parts in fp16, the result's rounding; scores: D products summed in fp32, half a step each of the largest sum of
+        # magnitudes, and the exponent's roundings.  While a row has no finite score its reference may be 2^14: D / 16 sums of that size more, half a step 2^-10 each.
+        mags = float((q.abs().amax(0) @ kh.abs().amax(0)) * D ** -0.5)
+        scores = 2 * ((D + 4) * 2.0 ** -24 * mags + D / 16 * 2.0 ** -10 * D ** -0.5) * mass
+        tol = 2.0 ** -7 * mass + scores + 2.0 ** -10 * mass.amax(-1, keepdim=True) + 2.0 ** -8 * ref.abs()
+        off = (O[:, h] - ref).abs()
+        assert bool((off <= tol)[~none].all()), (h, float((off / tol)[~none].nan_to_num(1e9).max()))
+        assert bool(torch.isnan(O[none, h]).all())
