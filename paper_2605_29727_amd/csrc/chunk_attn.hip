@@ -467,9 +467,9 @@ __device__ __forceinline__ void join_parts(const ChunkParams &p, int n, int sub,
                 if (i0 + b < n) {
                     const float w = __builtin_amdgcn_exp2f(ml[r][b].x - mn), wa = w * ml[r][b].z;
                     den[r] += w * ml[r][b].y;
-                    if (wa != 0.f)                      // (a part that the row sees none of has nothing to add)
+                    // (without a test of the weight: a part that the row sees none of is all zeros, and one whose weight vanishes hands on what is no number, as it would uncut)
 #pragma unroll
-                        for (int e = 0; e < E; ++e) acc[r][e] = fmaf(wa, (float)part[r][b][e], acc[r][e]);
+                    for (int e = 0; e < E; ++e) acc[r][e] = fmaf(wa, (float)part[r][b][e], acc[r][e]);
                 }
         }
     }

@@ -55,3 +55,31 @@ def test_infinite_keys(Hq, Hkv, D, L, M, tiles, low):
         off = (O[:, h] - ref).abs()
         assert bool((off <= tol)[~none].all()), (h, float((off / tol)[~none].nan_to_num(1e9).max()))
         assert bool(torch.isnan(O[none, h]).all())
+
+
+@pytest.mark.parametrize("kv,Hq,Hkv,D", [("bf16", 8, 2, 128), ("bf16", 8, 2, 64), ("fp8", 8, 2, 128), ("bf16", 32, 8, 128)], ids=["bf16_d128", "bf16_d64", "fp8", "bf16_32_heads"])
+@pytest.mark.parametrize("L,M,strong,at", [(9000, 1, 100, 8000), (9000, 1, 8000, 100), (30000, 1, 15000, 29999), (9000, 17, 50, 8990), (9000, 17, 8000, 3), (3000, 100, 2900, 60), (12000, 60, 60, 11000),
+                                           (8192, 300, 8000, 77), (8192, 300, 77, 8100), (20, 2000, 3, 15)])
+def test_a_value_that_is_no_number_behind_a_weight_that_vanishes(kv, Hq, Hkv, D, L, M, strong, at):
+    """One key takes all of the weight; a value that is no number still reaches every row that sees it, in whatever part of the keys it lies, and no other channel."""
+    import torch
+    b = make(L + M, [L], [M], Hq, Hkv, D, kv)
+    q = b["Q"][0, 0].clone()
+    b["Q"][:] = q
+    page, row = int(b["table"][0, strong // PAGE]), strong % PAGE
+    # scores: 2^-x of the strong key's for all others with x above 200, past the smallest number of fp32
+    if kv == "fp8":
+        b["K"][page, row] = (q.float().sign() * 448).to(torch.float8_e4m3fn).view(torch.uint8)
+        b["Q"][:] *= 8
+    else:
+        b["K"][page, row] = (24 * q.float()).to(torch.bfloat16)
+    clean = run(b).double()
+    assert bool(torch.isfinite(clean).all())
+    put(b, "V", 0, [at], 5, 0x7F if kv == "fp8" else math.inf)
+    O = run(b).double()
+    other = torch.arange(D, device="cuda") != 5
+    sees = torch.arange(M, device="cuda") + L >= at
+    assert bool((~torch.isfinite(O[sees][..., 5])).all())
+    # (parts in fp16 beside their largest magnitude, which channel 5 no longer takes part in: as for values in hidden places)
+    limit = 2 * (2.0 ** -9 * clean.abs().amax(-1, keepdim=True) + 2.0 ** -8 * clean.abs())
+    assert bool(((O - clean).abs() <= limit)[..., other].all()) and torch.equal(O[~sees], clean[~sees])
