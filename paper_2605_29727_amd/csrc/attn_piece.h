@@ -1514,7 +1514,7 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
         }
         settle();
     }
-    if constexpr (CAUSAL) m_run = times(m_run, cf);
+    if constexpr (CAUSAL) m_run = fmaxf(times(m_run, cf), NEG_BIG);        // (what stands for no reference stays a number whatever the scale)
     LaneRow lrow;
     if constexpr (CAUSAL) lrow = chunk_row(rw * 32 + c); else lrow = lane_row(p, by * WR + rw * 32 + c, rows_g, g, rq_.q0);
     const bool rvalid = lrow.valid;

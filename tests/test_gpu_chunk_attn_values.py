@@ -3,7 +3,7 @@ import math
 
 import pytest
 
-from test_gpu_chunk_attn import PAGE, make, run
+from test_gpu_chunk_attn import PAGE, check, make, run
 
 pytestmark = pytest.mark.gpu
 
@@ -83,3 +83,13 @@ def test_a_value_that_is_no_number_behind_a_weight_that_vanishes(kv, Hq, Hkv, D,
     # (parts in fp16 beside their largest magnitude, which channel 5 no longer takes part in: as for values in hidden places)
     limit = 2 * (2.0 ** -9 * clean.abs().amax(-1, keepdim=True) + 2.0 ** -8 * clean.abs())
     assert bool(((O - clean).abs() <= limit)[..., other].all()) and torch.equal(O[~sees], clean[~sees])
+
+
+@pytest.mark.parametrize("scale", [1e10, 1e25])
+@pytest.mark.parametrize("kv,Hq,Hkv,D", [("fp8", 8, 8, 128), ("bf16", 8, 8, 128), ("bf16", 8, 8, 64), ("bf16", 8, 2, 128)], ids=["fp8", "bf16_d128", "bf16_d64", "bf16_groups"])
+@pytest.mark.parametrize("Ls,Ms", [([5, 900, 0, 0, 77, 3, 40, 2000], [1800, 0, 700, 129, 1000, 65, 1500, 333]), ([20000, 0], [700, 3500]), ([700], [100]), ([40, 6000, 1, 300, 2000], [33, 1, 257, 16, 65]),
+                                   ([113 * i % 900 for i in range(70)], [130 + 37 * i % 200 for i in range(70)])], ids=lambda x: "-".join(map(str, x[:5])))
+def test_small_queries_and_a_large_scale(kv, Hq, Hkv, D, Ls, Ms, scale):
+    """Scores are as ever; what stands for a row without a score, times the scale, is past the range of fp32, and some parts have rows that see none of their keys."""
+    b = make(sum(Ms), Ls, Ms, Hq, Hkv, D, kv, sharp=D ** -0.5 / scale)
+    check(b, run(b, scale=scale), scale=scale)
