@@ -236,6 +236,11 @@ __device__ __forceinline__ bool whole_blocks(const ChunkParams &p, Walk &k, Chun
     return most_sum <= most_length;
 }
 
+// Even parts of 64 rows (single tokens' aside) are weighed with 60 tiles for a block, not 14: where all blocks find a workgroup, the large number keeps them in parts, and in one piece where
+// parts would be hardly smaller (29 chunks of up to 96 behind 1313, 28 heads: 30.5 us with 14, so 24.7; 3 prompts of up to 3064: 21.9, 17.2).  Single tokens split at less (16 over up to 1094
+// keys, E4M3: 16.3 with 100, with 14 12.0), and shares would count long and short blocks alike (128 single tokens over 100 to 4000 keys, 8 KV heads, bf16: 147 with 60, with 14 130; E4M3 92.4,
+// 76.9; 700 over up to 8000, E4M3: 577, 517).
+constexpr int MORE_OF_PARTS = (60 - 14) * 32 * WHOLE;
 template <bool FEW, int WAVES>
 __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool leader, Chunk &c, int *counts)
 {
@@ -268,13 +273,14 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
             }
         k.step = 0;
         if (all_blocks <= p.teams && all_blocks > 0) {
+            const int more = FEW && !p.always_parts ? MORE_OF_PARTS : 0;
             // (not below what the work comes to for each, rounded down)
             int lo = max(p.least_part, (int)((float)(all - (i64)all_blocks * p.start) * (0.999f / 32) / (float)(p.weight * p.teams))), n = all_blocks;
             auto count = [&](int part) {
                 return __builtin_amdgcn_readlane(wave_sums(t ? blocks * parts_of(t, part, __builtin_amdgcn_rcpf((float)part)) : 0), 63) * p.Hkv;
             };
             // what parts save has to be worth their merge
-            if ((longest - lo) * 32 * p.weight < p.start / 4) lo = max(lo, longest);
+            if ((longest - lo) * 32 * p.weight < (p.start + more) / 4) lo = max(lo, longest);
             else {
                 int hi = longest;
                 while (lo < hi) {
@@ -282,7 +288,8 @@ __device__ __forceinline__ Walk share_out(const ChunkParams &p, int lane, bool l
                     if (count(mid) <= p.teams) hi = mid; else lo = mid + 1;
                 }
             }
-            if (p.always_parts || ((i64)lo * 32 * p.weight <= w && longest < 1 << 20)) {      // (beyond, a cut's place would leave 32 bits)
+            const i64 share = most((all + (i64)all_blocks * more + p.teams - 1) >> teams_log2, p.wmin + more);
+            if (p.always_parts || ((i64)lo * 32 * p.weight <= share && longest < 1 << 20)) {      // (beyond, a cut's place would leave 32 bits)
                 // A part takes its tiles' time, and a while of the merge: the longest block is through the earliest with parts of about the root of its tiles (that
                 // ratio, measured).  With the smallest parts that there are workgroups for, of 4 tiles or more, one token over 26907 keys, 2 KV heads, took 66.5 us
                 // (now 24); 2 over 20582, E4M3, 28.5 (17.8); a chunk behind 2468 11.8 (8.4).
@@ -639,12 +646,10 @@ Shape shape_of(int batch, int total_M, int M_max, int L_max, int G, int Hkv, int
 }
 bool cuts(int M_max, int L_max) { return (L_max + M_max + 31) / 32 > SMALL; }
 
-// What a row block costs besides its keys, in tiles of whole blocks: finding it, its first loads, its last steps and stores.  Parts, shares and whole blocks are weighed with
+// What a row block costs besides its keys, in tiles of whole blocks: finding it, its first loads, its last steps and stores.  Shares and whole blocks are weighed with
 // it.  The stamps say 8 to 12 tiles; that much and half or twice it are within 2 % on average of 120 calls.  With 128 rows 16 is the best (3 chunks of up to 232 behind 4322, 64 heads: 35.8 us
-// with 9, so 31.4; E4M3 with 22: 27 of up to 914 behind 623, 91.7, so 77.1).  64 rows are taken where all blocks find a workgroup: a large number keeps them in parts, and in
-// one piece where parts would be hardly smaller (29 chunks of up to 96 behind 1313, 28 heads: 30.5 with 14, so 24.7; 3 prompts of up to 3064: 21.9, 17.2); single
-// tokens split at less (16 over up to 1094 keys, E4M3: 16.3 with 100, with 14 12.0).
-int start_of(int wr, int D, bool few) { return few ? 14 : wr == 64 ? 60 : wr == 128 ? 16 : D == 64 ? 12 : 9; }
+// with 9, so 31.4; E4M3 with 22: 27 of up to 914 behind 623, 91.7, so 77.1).
+int start_of(int wr, int D) { return wr == 64 ? 14 : wr == 128 ? 16 : D == 64 ? 12 : 9; }
 
 // Single tokens of requests that have a place on the chip each: always parts.  (With up to four parts per place where the requests alone fill it: 43 requests of up to 2305 keys,
 // 8 KV heads, 23.7 us, with one 18.1; 43 of up to 5520, E4M3, 48.8 and 49.6.)
@@ -726,7 +731,7 @@ int chunk_attn(const void *Q, const void *Kpool, const void *Vpool, int num_bloc
     p.words = reinterpret_cast<MergeWords *>(w8 + BTV_WS_HEADER);
     const bool behind = sh.behind && cut;
     p.begun = behind ? reinterpret_cast<Begun *>(w8 + wl.begun) : nullptr;
-    p.start = start_of(wr, D, few) * 32 * WHOLE;
+    p.start = start_of(wr, D) * 32 * WHOLE;
     p.wmin = p.start + 8 * 32 * WHOLE;
     p.part_rows = wr;
     p.least_part = few ? LEAST_OF_FEW : LEAST_PART;
