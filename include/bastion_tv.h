@@ -444,7 +444,8 @@ int btv_paged_extend(const int32_t *prefix_len, const int32_t *n_new, const int3
  *   Qout         [total, Hq, D] of `dtype`; may be Q where q_stride = Hq * D
  *   Kcache, Vcache  [num_slots, Hkv, D] of `dtype`: the pools of a paged cache (num_slots = num_blocks *
  *                BTV_PAGE), or a contiguous one (slot = row).  They may not overlap Q, K or V.
- * fp8kv: dtype bf16, caches of E4M3 codes: x / scale, limited to +-448, to nearest even (NaN stays NaN).
+ * fp8kv: dtype bf16, caches of E4M3 codes: the fp32 quotient x / scale, limited to +-448, to nearest
+ * even (NaN stays NaN).
  * ws (optional) receives the data flag for a slot >= num_slots; that row is passed over.
  *
  * rope_frequencies -- HOST function: inv_freq [R/2] HOST and the factor.  w_i = theta^(-2i/R) is

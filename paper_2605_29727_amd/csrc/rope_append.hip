@@ -12,6 +12,7 @@
 
 namespace {
 
+struct Scale { float by, inv; };                       // and its reciprocal
 struct RopeParams {
     const void *Q, *K, *V;
     long long q_stride, k_stride, v_stride;            // elements between rows
@@ -22,7 +23,8 @@ struct RopeParams {
     long long num_slots;
     int total, Hq, Hkv, R, interleaved;
     int units, inv_units, rotated, heads_per_pass, slices;      // see rope_append_kernel
-    float factor, inv_k, inv_v;                        // E4M3 caches: 1 / scale
+    float factor;
+    Scale scale_k, scale_v;                            // E4M3 caches
 };
 
 // Eight neighbouring channels, 16 bytes of bf16 (32 of fp32), as they are loaded and as numbers.
@@ -48,8 +50,9 @@ template <typename T> __device__ __forceinline__ void numbers(const Eight<T> &e,
         for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(w[k] << 16); x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
     }
 }
-// (E4M3: times 1 / scale, limited to the largest code; no number stays none)
-template <typename C> __device__ __forceinline__ void store8(C *p, const float (&x)[8], float inv)
+// (E4M3: x / scale, limited to the largest code; no number stays none.  The product with the reciprocal is off by up to 1.5 of its last bits, which takes some quotients half way between two
+// codes to the wrong one; what is missing, in one fused step, times the reciprocal leaves it right to 2^-46 ahead of its one rounding.)
+template <typename C> __device__ __forceinline__ void store8(C *p, const float (&x)[8], Scale s)
 {
     if constexpr (std::is_same_v<C, uint8_t>) {
         uint32_t w[2];
@@ -57,7 +60,10 @@ template <typename C> __device__ __forceinline__ void store8(C *p, const float (
         for (int k = 0; k < 2; ++k) {
             float y[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { const float v = x[4 * k + i] * inv; y[i] = v > 448.f ? 448.f : v < -448.f ? -448.f : v; }
+            for (int i = 0; i < 4; ++i) {
+                const float q = x[4 * k + i] * s.inv, v = fmaf(-fmaf(q, s.by, -x[4 * k + i]), s.inv, q);       // (signs: -0 stays -0)
+                y[i] = q > 448.f ? 448.f : q < -448.f ? -448.f : v;
+            }
             w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
         }
         *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
@@ -111,7 +117,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeParams p)
         for (int e = slice * 64 + lane; e < p.Hkv * (D / 8); e += 64 * p.slices) {
             float x[8];
             numbers(load8(V + e * 8), x);
-            store8(Vc + e * 8, x, p.inv_v);
+            store8(Vc + e * 8, x, p.scale_v);
         }
     float sn[ANGLES], cs[ANGLES];
     if (live && turns_) {
@@ -150,11 +156,11 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeParams p)
             }
         }
         if (isq) {
-            store8(Qo + h * D + c0, x, 1.0f);
-            if (!SIDE && turns_) store8(Qo + h * D + c1, y, 1.0f);
+            store8(Qo + h * D + c0, x, Scale{});
+            if (!SIDE && turns_) store8(Qo + h * D + c1, y, Scale{});
         } else {
-            store8(Kc + (h - p.Hq) * D + c0, x, p.inv_k);
-            if (!SIDE && turns_) store8(Kc + (h - p.Hq) * D + c1, y, p.inv_k);
+            store8(Kc + (h - p.Hq) * D + c0, x, p.scale_k);
+            if (!SIDE && turns_) store8(Kc + (h - p.Hq) * D + c1, y, p.scale_k);
         }
     }
 }
@@ -211,7 +217,7 @@ RopeParams params(const void *Q, long long q_stride, const void *K, long long k_
     p.position = position; p.slot = slot; p.inv_freq = inv_freq; p.Qout = Qout; p.Kc = Kc; p.Vc = Vc;
     p.flag = static_cast<uint32_t *>(ws);
     p.num_slots = num_slots; p.total = total; p.Hq = Hq; p.Hkv = Hkv; p.R = R; p.interleaved = interleaved;
-    p.factor = factor; p.inv_k = p.inv_v = 1.0f;
+    p.factor = factor;
     return p;
 }
 
@@ -235,7 +241,7 @@ int btv_rope_append_fp8kv(const void *Q, long long q_stride, const void *K, long
     BTV_REQUIRE(k_scale >= 1e-37f && k_scale <= 1e37f && v_scale >= 1e-37f && v_scale <= 1e37f, "FP8 K/V scales must lie in [1e-37, 1e37]");
     RopeParams p = params(Q, q_stride, K, k_stride, V, v_stride, total, Hq, Hkv, position, slot, inv_freq, R, interleaved, factor, Qout, K8cache, V8cache,
                           num_slots, ws);
-    p.inv_k = 1.0f / k_scale; p.inv_v = 1.0f / v_scale;
+    p.scale_k = { k_scale, 1.0f / k_scale }; p.scale_v = { v_scale, 1.0f / v_scale };
     return rope_append(p, BTV_BF16, 1, D, stream);
 }
 

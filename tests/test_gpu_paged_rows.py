@@ -360,3 +360,21 @@ def test_rope_append_refuses_caches_without_heads_or_channels(T, Hkv, D):
         cache = torch.zeros((2, PAGE, Hkv, D), dtype=dt, device="cuda")
         with pytest.raises((btv.BtvError, AssertionError)):       # (the library's refusal, or that such heads do not lie side by side)
             append(q, kv, kv, i, i, f, torch.zeros_like(q), cache, cache.clone(), *more)
+
+
+@pytest.mark.parametrize("scale", [7 / 512, 15 / 1024, 13 / 1024, 1.0, 0.013, 3e-5, 1234.567, 1e-37, 1e37])
+def test_rope_append_fp8_rounds_the_quotient(scale):
+    """Every bf16 number, without rotation: the code nearest to x / scale, ties to even; a product with 1 / scale takes a neighbour of some ties."""
+    import torch
+    from paper_2605_29727_amd import binding as btv
+    x = torch.arange(2**16, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(-1, 4, 64)
+    n = x.shape[0]
+    f = torch.tensor(scale, dtype=torch.float32)
+    want = (x.float() / f).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+    i = torch.arange(n, dtype=torch.int32, device="cuda")
+    X = x.cuda()
+    Kc, Vc = (torch.zeros((n, 4, 64), dtype=torch.uint8, device="cuda") for _ in range(2))
+    btv.btv_rope_append_fp8kv(X, X, X, i, i, torch.empty(0, dtype=torch.float64, device="cuda"), torch.empty_like(X), Kc, Vc, scale, scale)
+    number = ~torch.isnan(x)
+    for c in (Kc.cpu(), Vc.cpu()):
+        assert torch.equal(c[number], want[number]) and bool((c[~number] & 0x7F == 0x7F).all())
