@@ -436,7 +436,8 @@ int btv_paged_extend(const int32_t *prefix_len, const int32_t *n_new, const int3
  *   a' = factor * (a cos t - b sin t),  b' = factor * (a sin t + b cos t);
  * channels from R on stay as they are.  t is formed and reduced in fp64, the rotation is in fp32.
  *   Q, K, V      rows of [Hq, D], [Hkv, D], [Hkv, D] of `dtype`, q_stride, k_stride, v_stride ELEMENTS
- *                apart (a projection's packed output is read where it lies); 16-byte aligned rows
+ *                apart (a projection's packed output is read where it lies); 16-byte aligned rows,
+ *                total <= 2^26 - 4 of them
  *   position, slot  [total], as paged_extend writes them.  Rows of a slot < 0 are not stored in the
  *                cache (their queries are rotated all the same).  No two rows may have one slot: it
  *                would hold either row, or parts of both.

@@ -12,6 +12,8 @@
 
 namespace {
 
+constexpr int MOST_ROWS = (1 << 26) - 4;               // (a wavefront each; a launch has fewer than 2^32 threads)
+
 struct Scale { float by, inv; };                       // and its reciprocal
 struct RopeParams {
     const void *Q, *K, *V;
@@ -168,7 +170,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeParams p)
 int rope_append(RopeParams p, int dtype, int eb, int D, void *stream)
 {
     BTV_REQUIRE(dtype == BTV_F32 || dtype == BTV_BF16, "dtype=%d unsupported", dtype);
-    BTV_REQUIRE(p.total >= 0, "total=%d out of range", p.total);
+    BTV_REQUIRE(p.total >= 0 && p.total <= MOST_ROWS, "total=%d outside [0,%d]", p.total, MOST_ROWS);
     BTV_REQUIRE(p.Hq >= 1 && p.Hkv >= 1 && p.Hq <= 1024 && p.Hkv <= 1024, "bad heads Hq=%d Hkv=%d", p.Hq, p.Hkv);
     BTV_REQUIRE(D == 64 || D == 128, "D=%d not in {64,128}", D);
     BTV_REQUIRE(p.R >= 0 && p.R <= D && p.R % 16 == 0, "R=%d: a multiple of 16 up to D=%d", p.R, D);

@@ -50,6 +50,12 @@ def test_rope_append_refuses(change, text):
     refused("btv_rope_append", rope_args(**change), text)
 
 
+@pytest.mark.parametrize("total", [(1 << 26) - 3, 1 << 30, 2**31 - 1])
+def test_rope_append_refuses_more_rows_than_a_launch_has(total):
+    refused("btv_rope_append", rope_args(total=total), "total")
+    refused("btv_rope_append_fp8kv", rope_args(True, total=total), "total")
+
+
 @pytest.mark.parametrize("scale", [0.0, -1.0, math.nan, math.inf, 1e-38])
 def test_rope_append_fp8_refuses_scales(scale):
     refused("btv_rope_append_fp8kv", rope_args(True, k_scale=C.c_float(scale)), "scales")
