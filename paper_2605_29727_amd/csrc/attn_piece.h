@@ -402,14 +402,18 @@ __device__ __forceinline__ void exp_half(const f32x16 &x, int mm, bf16x8 &pbm, f
 // the scores arrive relative to it and a probability is exp2 of the accumulator as it stands.  The reference only moves where
 // the tile's maximum exceeds it by more than LAZY, so that probabilities stay below 2^LAZY and most tiles rescale nothing; the
 // result is the same, numerator and denominator refer to the same m_run.  Where it moves the tile's scores are shifted by hand.
+// whole: all rows see all of the tile.  A row that has no score above -infinity there has no reference for the tiles behind it, which do not look for one: it starts
+// from -NO_SCORE, far below any maximum, so that its first finite score makes a tile's sum overflow and the tile be done again, and near enough to leave that tile's scores
+// 2^-10.  (A row that has met none by the end: attn_piece, behind its loops.)
+constexpr float NO_SCORE = 16384.0f;
 template <int DT, typename C>
-__device__ __forceinline__ void rebase_tile(f32x16 &srel, float &base, f32x16 &negb, float &m_run, float &l_run, f32x16 (&oacc)[DT], C c)
+__device__ __forceinline__ void rebase_tile(f32x16 &srel, float &base, f32x16 &negb, float &m_run, float &l_run, f32x16 (&oacc)[DT], C c, bool whole)
 {
     constexpr float LAZY = 8.0f;
     const float rmax = tile_max(srel);
-    const bool grow = times((rmax + base) - m_run, c) > LAZY;
-    if (__builtin_amdgcn_ballot_w64(grow) != 0ull) {
-        const float mnew = grow ? rmax + base : m_run;
+    const bool grow = times((rmax + base) - m_run, c) > LAZY, none = whole && m_run < 0.5f * NEG_BIG;
+    if (__builtin_amdgcn_ballot_w64(grow || none) != 0ull) {
+        const float mnew = grow ? rmax + base : none ? -NO_SCORE : m_run;
         const float alpha = __builtin_amdgcn_exp2f(times(m_run - mnew, c));
         m_run = mnew;
         l_run *= alpha;
@@ -432,15 +436,15 @@ __device__ __forceinline__ void rebase_tile(f32x16 &srel, float &base, f32x16 &n
 constexpr float GROW = 1048576.0f;       // 2^20: a sum of 16 terms above it means some score > 16
 template <int DT, typename C>
 __device__ __forceinline__ void probabilities(f32x16 &x, bool exact, float &base, f32x16 &negb, float &m_run, float &l_run, f32x16 (&oacc)[DT],
-                                              bf16x8 (&pb)[2], C c)
+                                              bf16x8 (&pb)[2], C c, bool whole)
 {
-    if (exact) rebase_tile<DT>(x, base, negb, m_run, l_run, oacc, c);
+    if (exact) rebase_tile<DT>(x, base, negb, m_run, l_run, oacc, c, whole);
     float ts[2] = { 0.f, 0.f };
     exp_half(x, 0, pb[0], ts[0], c);
     exp_half(x, 1, pb[1], ts[1], c);
     float sum = ts[0] + ts[1];
     if (!exact && __builtin_amdgcn_ballot_w64(!(sum <= GROW)) != 0ull) {
-        rebase_tile<DT>(x, base, negb, m_run, l_run, oacc, c);
+        rebase_tile<DT>(x, base, negb, m_run, l_run, oacc, c, false);
         ts[0] = ts[1] = 0.f;
         exp_half(x, 0, pb[0], ts[0], c);
         exp_half(x, 1, pb[1], ts[1], c);
@@ -539,7 +543,7 @@ __device__ __forceinline__ void do_tile(uint32_t stage, int kb, int Lr, int l, S
     f32x16 s = qk_tile<DS>(ka, qreg, negb);
     if (!PLAIN && kb + 32 > Lr) mask_tile(s, vis_word(seen, kb, Lr), l >> 5);
     bf16x8 pb[2];
-    probabilities<DT>(s, !PLAIN && exact, base, negb, m_run, l_run, oacc, pb, c);
+    probabilities<DT>(s, !PLAIN && exact, base, negb, m_run, l_run, oacc, pb, c, kb + 32 <= Lr);
     lds_wait_vt<DT>(va);
     if constexpr (!PLAIN && std::is_same_v<Seen, LastKey>)
         if (kb + 32 > Lr && take_out<DT>(va)) seen.odd = true;
@@ -641,7 +645,7 @@ __device__ __forceinline__ void do_tile8(uint32_t stage, int kb, int Lr, int l, 
     }
     if (!PLAIN && kb + 32 > Lr) mask_tile(s, vis_word(seen, kb, Lr), l >> 5);
     bf16x8 pb[2];
-    probabilities<DT>(s, !PLAIN && exact, base, negb, m_run, l_run, oacc, pb, c);
+    probabilities<DT>(s, !PLAIN && exact, base, negb, m_run, l_run, oacc, pb, c, kb + 32 <= Lr);
     lds_wait_vt8(v8);
     if constexpr (!PLAIN && std::is_same_v<Seen, LastKey>)
         if (kb + 32 > Lr && take_out8<DT>(v8)) seen.odd = true;
@@ -1137,16 +1141,6 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
 #pragma unroll
         for (int v = 0; v < 16; ++v) oacc[dt][v] = 0.f;
 
-    // A row whose first tile has no score above -infinity has no reference for the tiles behind it, which do not look for one.  It starts from -NO_SCORE: far below any
-    // maximum, so that its first finite score makes the tile's sum overflow and the tile be done again, and near enough to leave that tile's scores 2^-10.
-    // settle(): a row that has met none by the end has none, and whatever it is merged with is above it.
-    constexpr float NO_SCORE = 16384.0f;
-    auto settle = [&]() {
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(m_run == -NO_SCORE) != 0ull, 0)) {       // (rare; a maximum of just that has a sum)
-            const float sum = l_run + __shfl_xor(l_run, 32);
-            if (m_run == -NO_SCORE && sum == 0.f) m_run = NEG_BIG;
-        }
-    };
     bf16x8 qreg[DS];
     if constexpr (DS == 8)
         asm volatile("s_waitcnt lgkmcnt(0)"
@@ -1297,7 +1291,7 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
                 read_k_half_at<D, 1>(kbase, kh); wait_k_half<KH, 0>(kh); x = qk_half<DS, 1>(kh, qreg, x);
                 read_k_half_at<D, 0>(kbase + slot_off(1), kh);
                 negm = -tile_max(x);
-                negm = negm <= FLT_MAX ? negm : NO_SCORE;
+                negm = negm <= FLT_MAX ? negm : NO_SCORE;        // (a row of which this tile's scores all are -infinity: see rebase_tile)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) x[v] += negm;
                 exp_half(x, 0, pa[0], l_run, cf);                // x <= 0 here: no growth check
@@ -1413,7 +1407,6 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
                 wait_v_half<DT, 0>(vh);
                 pv_half<DT>(vh, pn[1], oacc);
                 m_run = -negm;
-                settle();
             };
             // One iteration per trip, the new probabilities copied into place at its end (8 moves): with the roles of
             // two register sets alternating over an unrolled pair the allocator shuffles tuples and spills.
@@ -1445,10 +1438,10 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
             j0 = Tf;
         }
         // ---- the remaining tiles (those that touch tree rows, or all of a short split), step by step ----
-        if (j0 > 0) {                                            // (m_run is a maximum after the pipelined part, if there was a finite score)
-            base = m_run > 0.5f * NEG_BIG ? m_run : 0.f;
+        if (j0 > 0) {                                            // (m_run is a maximum after the pipelined part, or -NO_SCORE)
+            base = m_run;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) negb[v] = -base;
+            for (int v = 0; v < 16; ++v) negb[v] = -m_run;
         }
         read_mask();                                             // (barriers since the sets were written: those of the prologue)
         for (int j = j0; j < st1 - st0; ++j) {
@@ -1485,15 +1478,7 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
         };
         // Rounds that ask for KW tiles of the prefix with all their keys, and so only take such, have nothing to test for.
         const int plain = min(st1, Lr / 32);
-        if (live && st + kwu < st1) {                            // (on its own: nothing has to be cleared ahead of it)
-            tile(std::false_type{});
-            if (__builtin_expect((st + kwu) * 32 + 32 <= Lr && __builtin_amdgcn_ballot_w64(m_run < 0.5f * NEG_BIG) != 0ull, 0)) {       // (rare)
-                const bool none = m_run < 0.5f * NEG_BIG;
-                if (none) m_run = base = -NO_SCORE;
-#pragma unroll
-                for (int v = 0; v < 16; ++v) negb[v] = none ? NO_SCORE : negb[v];
-            }
-        }
+        if (live && st + kwu < st1) tile(std::false_type{});     // (on its own: nothing has to be cleared ahead of it)
         next_round();
         whole_tiles();
         for (; issued + KW <= plain; next_round()) {
@@ -1512,7 +1497,11 @@ __device__ __forceinline__ void attn_piece(const AttnParams &p, unsigned char *s
             begin_round(st);
             if (live && st + kwu < st1) tile(std::false_type{});
         }
-        settle();
+    }
+    // A row that has met no score above -infinity has no reference, and whatever it is merged with is above it.
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(m_run == -NO_SCORE) != 0ull, 0)) {        // (rare; a maximum of just that has a sum)
+        const float sum = l_run + __shfl_xor(l_run, 32);
+        if (m_run == -NO_SCORE && sum == 0.f) m_run = NEG_BIG;
     }
     if constexpr (CAUSAL) m_run = fmaxf(times(m_run, cf), NEG_BIG);        // (what stands for no reference stays a number whatever the scale)
     LaneRow lrow;
