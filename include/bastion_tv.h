@@ -480,8 +480,16 @@ int btv_rope_frequencies(int R, double theta, int scaling, double stretch, doubl
  *        btv_tree_verify_attn_paged; 1 <= batch <= 4096
  *   M_max, L_max  HOST upper bounds of a request's new rows (1 <= M_max <= 2^20) and of its prefix; a
  *        request that exceeds them, or max_blocks * BTV_PAGE, is passed over and flagged
+ * Scores, sums and accumulators are fp32.  Probabilities enter the product with V, and the row's sum,
+ * rounded to bf16; where a row's keys are shared out, each part of its result travels as fp16 beside the
+ * part's largest magnitude.  Both are within the rounding of O (2.0 to 2.4e-3 of the result by the
+ * 2-norm, 1.7e-3 for the result rounded once).  Scores come to the exponential with fp32's relative 2^-24
+ * per product: scaled scores above 2^17 or so are no longer right to 2^-7 of a weight, and Q.K itself has
+ * to stay below 1e29.  Keys and values that a row does not see do not reach it, whatever is in them; a
+ * score of -infinity weighs nothing.
  * The workspace is of the attention kind; the query answers what every call with no larger batch,
- * M_max and L_max needs.  fp8kv: as there, D = 128. */
+ * M_max and L_max needs.  fp8kv: as there, D = 128 (rope_append_fp8kv also writes caches of D = 64, for
+ * readers of the caller's own). */
 size_t btv_chunk_attn_paged_workspace(int batch, int M_max, int L_max, int Hq, int Hkv, int D);
 int btv_chunk_attn_paged(const void *Q, const void *Kpool, const void *Vpool, int num_blocks,
                          const int32_t *block_table, int max_blocks, const int32_t *q_offset,

@@ -363,7 +363,7 @@ def btv_kv_commit_paged(Kpool, Vpool, block_table, prefix_len, path, n_acc, new_
 def btv_paged_extend(prefix_len, n_new, depth, n_pages, free_pages, n_free, block_table, q_offset, slot, position, n_pages_out, n_free_out,
                      ws=None) -> None:
     """Pages, slots and positions of the requests' next rows.  block_table [batch, max_blocks] is extended in place; free_pages has an entry per page of the
-    cache; slot and position may be longer than the rows are (a padded batch: slot -1 there)."""
+    cache; slot and position may be longer than the rows are (a padded batch: slot -1 there), depth then as well: the host does not know how many rows there are."""
     (_face or _load_face()).paged_extend(prefix_len, n_new, depth, n_pages, free_pages, n_free, block_table, q_offset, slot, position, n_pages_out, n_free_out, ws)
 
 

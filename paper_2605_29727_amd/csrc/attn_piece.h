@@ -480,7 +480,7 @@ __device__ __forceinline__ void mask_tile(f32x16 &s, uint32_t vis, int h)
 
 // Values that are not numbers, in a tile of which some rows see a part only: a probability of 0 times such a value would reach the rows that do
 // not see its key.  They are taken out of the operands, and the wavefront remembers that it has met one (rare; found by a product with 0, two values at a time): what they
-// do to the rows that see them is added at the end (odd_values).
+// do to the rows that see them is added at the end of attn_piece.
 template <int DT>
 __device__ __forceinline__ bool take_out(bf16x4 (&va)[DT][2][2])
 {

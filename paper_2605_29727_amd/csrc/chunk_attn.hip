@@ -15,9 +15,9 @@
 // Neighbouring shares are on one XCD, which so keeps to one KV head or two, whose K/V its workgroups meet in their L2.  Where there are fewer blocks than workgroups, blocks go
 // in even parts instead, and where there are more, but a few for each workgroup at most and of lengths that come out even, whole blocks in turns.
 //
-// A chunk of 2048 tokens behind 30720, 64 heads of 128 (8 of K/V): 1.83 ms, 1.16 PFLOP/s (a bf16 product of 8192^3: 1.40), behind 8192 with 32 heads 295 us, 1.05; of a tile's
-// 0.93 us the matrix instructions alone take 0.6 to 0.7 at the clock that they leave, the exponentials and the LDS reads the rest.  32 tokens over 100 to 4000 keys,
-// E4M3, 51 MB: 19 us.  Blocks of few tiles are bound by a piece's ends (us, 256 rows of 128): finding it 1.4, the first loads 2 to 3, the first scores 1.2, the last products
+// A chunk of 2048 tokens behind 30720, 64 heads of 128 (8 of K/V): 1.81 ms, 1.18 PFLOP/s (a bf16 product of 8192^3: 1.40), behind 8192 with 32 heads 292 us, 1.06 (7 % more
+// on some cards); of a tile's 0.93 us the matrix instructions alone take 0.6 to 0.7 at the clock that they leave, the exponentials and the LDS reads the rest.  32 tokens over 100 to 4000 keys,
+// E4M3, 51 MB: 18.4 us.  Blocks of few tiles are bound by a piece's ends (us, 256 rows of 128): finding it 1.4, the first loads 2 to 3, the first scores 1.2, the last products
 // 1.1, the masked tiles 1.5, the last sums 1.4, stores 1.
 #include "attn_piece.h"
 
@@ -498,7 +498,8 @@ __device__ __forceinline__ int part_at(const ChunkParams &p, int first, int i)
 // The workgroup that stores the last of a block's parts merges them all (each counts itself in, at the block's first share; the count is back at 0 then).  Nothing waits: who is
 // not last goes on.  Rows and the count go to the memory side and come from there, where all XCDs see the same (a store is acknowledged when it is there, and only
 // then its workgroup counts itself in); with fences of the device in their place every workgroup would write its XCD's L2 back and drop what it holds of others'
-// memory.  32 single tokens, E4M3, up to 4000 keys: 25.4 us with fences, 18.8 so, 21.3 with a second launch that merges.  With 64 and 128 rows, by a second launch
+// memory.  (Rows and the count are accessed at the scope of the device, and the rows' stores are waited for ahead of the count: that order is all that a release
+// and an acquire would add for such accesses on this chip.)  32 single tokens, E4M3, up to 4000 keys: 25.4 us with fences, 18.8 so, 21.3 with a second launch that merges.  With 64 and 128 rows, by a second launch
 // and so: 4 prompts of up to 1999, 32 heads of 64 (nothing is cut): 24.5, 23.0; 11 chunks of up to 361 behind 830, 8 heads of 64: 16.8, 14.2.  With 256 one CU reads 64 KB a part: 6 prompts
 // of up to 1104, 32 heads of 64: 20.4, 18.0; 8 requests of 1 to 600 rows behind up to 16384: 62.3, 64.3; a chunk of 2048 behind 8192: 286.8, 290.8 (one by one 334, 351).  There the launch
 // stays where each workgroup has more than 30 tiles' work.

@@ -6,7 +6,7 @@
 // one launch, in which no workgroup waits for another.  Then a workgroup writes its share of the rows, one thread per row (the
 // request found by bisection in LDS, the page either from the table or straight from the free list, so that nothing waits for the table's new entries
 // either), and its share of the requests' new table entries.  Latency bounds it: the launch, the lengths' round trip, the pages' round trip.  8 trees 4.7 us, 700 requests with
-// 1 to 500 new rows each (57600 rows) 5.5 us; with the requests' numbers in memory, not LDS, 6.4.
+// 1 to 500 new rows each (57600 rows) 5.5 us (with the requests' numbers in memory, not LDS, 6.4).
 #include "btv_common.h"
 
 #include <atomic>
